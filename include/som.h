@@ -47,6 +47,8 @@ enum { SOM_FILTER_FP32 = 0, SOM_FILTER_SPLIT_F16 = 1, SOM_FILTER_TWO_LEVEL = 2, 
 enum { SOM_NEIGHBORHOOD_GAUSSIAN = 0, SOM_NEIGHBORHOOD_BUBBLE = 1 };   /* option -n               */
 enum { SOM_SMOOTH_AUTO = 0, SOM_SMOOTH_VECTOR = 1, SOM_SMOOTH_MATRIX = 2, SOM_SMOOTH_MATRIX_SPLIT = 3 };   /* see som_set_smoothing */
 
+enum { SOM_FP32 = 0, SOM_FP16 = 1, SOM_BF16 = 2 };        /* element types, see som_mx4_quantize */
+
 /* Neighbourhood mass below which a node keeps its weights (see som_train_epoch_dense). */
 #define SOM_EPS_MASS 1e-20
 
@@ -166,6 +168,73 @@ int som_update_csr(som_ctx *ctx, const int64_t *indptr, const int32_t *indices, 
 int som_set_data_dense(som_ctx *ctx, const float *data, int64_t n);
 int som_set_data_csr(som_ctx *ctx, const int64_t *indptr, const int32_t *indices,
                      const float *values, int64_t n, int64_t nnz);
+
+/*
+ * Microscaled 4-bit rows - the third kind of data, for training sets that would not fit otherwise (the paper names
+ * memory as the first constraint) and for maps that are searched often: 17 bytes for 32 features instead of 128, and the
+ * matrix cores multiply them at four times the rate of fp16.
+ *   A row of dim features is B = ceil(dim / 32) blocks of 32 consecutive features.
+ *   codes   device [n][16 B] bytes, aligned to 16: element 2 i of a block in the low four bits of its byte i,
+ *           element 2 i + 1 in the high ones.  A sign bit over a magnitude 0..7 that stands for 0, 0.5, 1, 1.5, 2, 3,
+ *           4, 6.  Elements past dim in the last block must be zero.
+ *   scales  device [n][B] bytes: byte s multiplies its block by 2^(s - 127); s = 255: every element of the block is NaN.
+ * Rows lie behind one another (no row stride).  NULL or unaligned codes, NULL scales, n outside [1, 2^31) ->
+ * SOM_ERR_INVALID_ARG.
+ *
+ * som_mx4_quantize - rows into this form.
+ *   rows    device [n] rows of dim elements of `type` (SOM_FP32, SOM_FP16, SOM_BF16), `stride` elements apart
+ *           (>= dim; any value if n = 1), read only.
+ *   A block's scale is 2^(floor(log2 of its largest magnitude) - 2), at least 2^-127; its elements are divided by
+ *   it and rounded to the nearest value, ties to the one with an even code; above 6 they become 6 (so the largest elements of a block may lose
+ *   up to a quarter).  Zeros of either sign keep it.  A block with an infinity or a NaN becomes NaN (scale 255, codes 0); a block of
+ *   zeros has scale byte 0.
+ * som_mx4_dequantize - the values that rows of this form stand for, rounded once to `type` (exact for fp32 and
+ *   bf16, but for magnitudes beyond their range; fp16 has subnormal values and infinity outside its own).
+ *   rows    device, written: [n] rows of dim elements, `stride` apart; what lies between the rows is left as it is.
+ * Errors of both: unknown type, stride < dim or >= 2^40 (n > 1), rows not aligned to their type -> SOM_ERR_INVALID_ARG.
+ */
+int som_mx4_quantize(som_ctx *ctx, const void *rows, int type, int64_t n, int64_t stride, uint8_t *codes, uint8_t *scales);
+int som_mx4_dequantize(som_ctx *ctx, const uint8_t *codes, const uint8_t *scales, int64_t n, void *rows, int type,
+                       int64_t stride);
+
+/*
+ * som_mx4_product - the dot products of all pairs of two sets of microscaled 4-bit rows (the response of every node to every
+ * instance, if b is a code book): out[i][j] = sum over the features of a_i and b_j.
+ *   codes_a, scales_a, n; codes_b, scales_b, m   the rows, of the context's dim, read only.
+ *   out     device [n] rows of m elements of `type`, `stride` elements apart (>= m; any value if n = 1); what lies between
+ *           the rows is left as it is.
+ * Products of two blocks are exact; their sum is taken in fp32 (each addition cuts off below 2^-23 of its largest
+ * term) and rounded once to the type.  A NaN block of either row makes the product NaN.
+ * Errors: as above, for out as for rows there.
+ */
+int som_mx4_product(som_ctx *ctx, const uint8_t *codes_a, const uint8_t *scales_a, int64_t n, const uint8_t *codes_b,
+                    const uint8_t *scales_b, int64_t m, void *out, int type, int64_t stride);
+
+/*
+ * som_bmus_mx4 - som_bmus_dense for microscaled 4-bit rows and a code book in the same form.
+ *   node_codes, node_scales   the rows*cols nodes (som_mx4_quantize of a code book, made once for a map that is searched
+ *           often), read only.
+ *   bmus    device [n] int32 out: the node whose values are nearest to those of the instance, exact ties to the lowest index.
+ * Decided by the distances of the values that both sides stand for: exactly, while the scales of a row's products
+ * lie within a factor of 2^40 of each other, beyond that in fp64.  An instance with a NaN block is mapped to node 0, a
+ * node with one is never chosen.
+ *
+ * som_update_mx4, som_train_epoch_mx4, som_set_data_mx4 - the batch update, one epoch, and the registration of a
+ * training set for som_train and som_train_snapshots, as for dense data.  The code book stays fp32; the search of an
+ * epoch quantises it to this form first, so that an epoch's BMUs are those of som_bmus_mx4 against som_mx4_quantize of the incoming
+ * code book.  The sums are those of the values that the rows stand for.
+ * Scratch: 17/32 of a byte per weight of the code book (epochs), and per instance of a search up to 128 bytes.  It grows without
+ * waiting: what it replaces is kept until som_destroy.  A call that is being recorded into a graph and needs more than
+ * any call before it -> SOM_ERR_STATE, nothing enqueued.  (The update's own scratch is that of som_update_dense.)
+ * som_get_stats and som_two_level_stats do not cover these searches.
+ */
+int som_bmus_mx4(som_ctx *ctx, const uint8_t *codes, const uint8_t *scales, int64_t n, const uint8_t *node_codes,
+                 const uint8_t *node_scales, int32_t *bmus);
+int som_update_mx4(som_ctx *ctx, const uint8_t *codes, const uint8_t *scales, int64_t n, const int32_t *bmus,
+                   float *codebook, float radius, float scale);
+int som_train_epoch_mx4(som_ctx *ctx, const uint8_t *codes, const uint8_t *scales, int64_t n, float *codebook,
+                        float radius, float scale, int32_t *bmus);
+int som_set_data_mx4(som_ctx *ctx, const uint8_t *codes, const uint8_t *scales, int64_t n);
 
 /*
  * som_train - n_epochs epochs on the registered data with cooled radius and scale, all

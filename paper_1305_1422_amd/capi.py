@@ -20,6 +20,7 @@ SOM_GRID_SQUARE, SOM_GRID_HEXAGONAL = 0, 1
 SOM_COOL_AS_RADIUS, SOM_COOL_LINEAR, SOM_COOL_EXPONENTIAL = -1, 0, 1
 SOM_FILTER_FP32, SOM_FILTER_SPLIT_F16, SOM_FILTER_TWO_LEVEL, SOM_FILTER_AUTO = 0, 1, 2, 3
 SOM_NEIGHBORHOOD_GAUSSIAN, SOM_NEIGHBORHOOD_BUBBLE = 0, 1
+SOM_FP32, SOM_FP16, SOM_BF16 = 0, 1, 2
 SOM_SMOOTH_AUTO, SOM_SMOOTH_VECTOR, SOM_SMOOTH_MATRIX, SOM_SMOOTH_MATRIX_SPLIT = 0, 1, 2, 3
 
 EXPORTS = [
@@ -29,6 +30,8 @@ EXPORTS = [
     "som_update_dense", "som_update_csr",
     "som_set_data_dense", "som_set_data_csr", "som_train", "som_train_snapshots",
     "som_bmu_distances_dense", "som_bmu_distances_csr", "som_bmu_distances_dense_static",
+    "som_mx4_quantize", "som_mx4_dequantize", "som_mx4_product", "som_bmus_mx4", "som_update_mx4", "som_train_epoch_mx4",
+    "som_set_data_mx4",
     "som_cool_schedule", "som_umatrix", "som_get_stats", "som_two_level_stats",
     "som_profile_enable", "som_profile_read",
     "som_set_filter", "som_set_smoothing", "som_set_sparse_hot_block", "som_sparse_hot_block_active", "som_set_sparse_dense_filter", "som_sparse_dense_filter_active", "som_set_neighborhood", "som_set_scale_cooling", "som_validate_csr", "som_debug_scores_dense", "som_debug_scores_csr", "som_debug_select_margins", "som_debug_subspace", "som_debug_subspace_always", "som_debug_subspace_used", "som_debug_subspace_fine", "som_debug_subspace_csr", "som_debug_mfma_f16", "som_debug_xcc_ids",
@@ -88,6 +91,20 @@ def load():
     L.som_bmu_distances_csr.argtypes = [vp, vp, vp, vp, i64, i64, vp, vp, vp, vp]
     L.som_bmu_distances_dense_static.restype = i32
     L.som_bmu_distances_dense_static.argtypes = [vp, i64, i32, vp, i32, vp, vp, vp, vp]
+    L.som_mx4_quantize.restype = i32
+    L.som_mx4_quantize.argtypes = [vp, vp, i32, i64, i64, vp, vp]
+    L.som_mx4_dequantize.restype = i32
+    L.som_mx4_dequantize.argtypes = [vp, vp, vp, i64, vp, i32, i64]
+    L.som_mx4_product.restype = i32
+    L.som_mx4_product.argtypes = [vp, vp, vp, i64, vp, vp, i64, vp, i32, i64]
+    L.som_bmus_mx4.restype = i32
+    L.som_bmus_mx4.argtypes = [vp, vp, vp, i64, vp, vp, vp]
+    L.som_update_mx4.restype = i32
+    L.som_update_mx4.argtypes = [vp, vp, vp, i64, vp, vp, f32, f32]
+    L.som_train_epoch_mx4.restype = i32
+    L.som_train_epoch_mx4.argtypes = [vp, vp, vp, i64, vp, f32, f32, vp]
+    L.som_set_data_mx4.restype = i32
+    L.som_set_data_mx4.argtypes = [vp, vp, vp, i64]
     L.som_umatrix.restype = i32
     L.som_umatrix.argtypes = [vp, vp, vp]
     L.som_get_stats.restype = i32
@@ -153,6 +170,34 @@ def _ptr(t, dtype, name: str, allow_none: bool = False):
     if not t.is_contiguous():
         raise TypeError(f"{name} must be contiguous")
     return C.c_void_p(t.data_ptr())
+
+
+def _typed(t, name: str, columns: Optional[int] = None):
+    """(pointer, element type, row stride) of a matrix whose rows may lie apart."""
+    import torch
+    types = {torch.float32: SOM_FP32, torch.float16: SOM_FP16, torch.bfloat16: SOM_BF16}
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA/ROCm torch tensor (device memory)")
+    if t.dtype not in types:
+        raise TypeError(f"{name} must have dtype float32, float16 or bfloat16, got {t.dtype}")
+    if t.dim() != 2:
+        raise TypeError(f"{name} must have two dimensions")
+    if columns is not None and t.shape[1] != columns:
+        raise ValueError(f"{name} must have {columns} columns, got {t.shape[1]}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise TypeError(f"{name} must be contiguous within its rows")
+    return C.c_void_p(t.data_ptr()), types[t.dtype], t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _mx4(codes, scales, name: str):
+    """(codes pointer, scales pointer, rows) of microscaled 4-bit rows."""
+    import torch
+    pc, ps = _ptr(codes, torch.uint8, f"{name} codes"), _ptr(scales, torch.uint8, f"{name} scales")
+    if codes.dim() != 2 or scales.dim() != 2:
+        raise TypeError(f"{name} codes and scales must have two dimensions")
+    if codes.shape[0] != scales.shape[0] or codes.shape[1] != 16 * scales.shape[1]:
+        raise ValueError(f"{name} codes must be [n][16 B] where scales are [n][B], got {tuple(codes.shape)} and {tuple(scales.shape)}")
+    return pc, ps, codes.shape[0]
 
 
 def _check(ctx, rc: int):
@@ -245,6 +290,57 @@ def som_set_data_csr(ctx, indptr, indices, values) -> None:
                                         _ptr(indices, torch.int32, "indices", True),
                                         _ptr(values, torch.float32, "values", True), indptr.shape[0] - 1,
                                         0 if indices is None else indices.shape[0]))
+
+
+def som_mx4_quantize(ctx, rows, codes, scales) -> None:
+    pr, kind, stride = _typed(rows, "rows")
+    pc, ps, n = _mx4(codes, scales, "the")
+    if n != rows.shape[0] or scales.shape[1] != (rows.shape[1] + 31) // 32:
+        raise ValueError("codes and scales do not fit the rows")
+    _check(ctx, load().som_mx4_quantize(ctx, pr, kind, n, stride, pc, ps))
+
+
+def som_mx4_dequantize(ctx, codes, scales, rows) -> None:
+    pr, kind, stride = _typed(rows, "rows")
+    pc, ps, n = _mx4(codes, scales, "the")
+    if n != rows.shape[0] or scales.shape[1] != (rows.shape[1] + 31) // 32:
+        raise ValueError("codes and scales do not fit the rows")
+    _check(ctx, load().som_mx4_dequantize(ctx, pc, ps, n, pr, kind, stride))
+
+
+def som_mx4_product(ctx, codes_a, scales_a, codes_b, scales_b, out) -> None:
+    pa, sa, n = _mx4(codes_a, scales_a, "a's")
+    pb, sb, m = _mx4(codes_b, scales_b, "b's")
+    po, kind, stride = _typed(out, "out", m)
+    if out.shape[0] != n or scales_a.shape[1] != scales_b.shape[1]:
+        raise ValueError("a, b and out do not fit each other")
+    _check(ctx, load().som_mx4_product(ctx, pa, sa, n, pb, sb, m, po, kind, stride))
+
+
+def som_bmus_mx4(ctx, codes, scales, node_codes, node_scales, bmus) -> None:
+    import torch
+    pc, ps, n = _mx4(codes, scales, "the")
+    pw, sw, _ = _mx4(node_codes, node_scales, "the nodes'")
+    _check(ctx, load().som_bmus_mx4(ctx, pc, ps, n, pw, sw, _ptr(bmus, torch.int32, "bmus")))
+
+
+def som_update_mx4(ctx, codes, scales, bmus, codebook, radius: float, scale: float) -> None:
+    import torch
+    pc, ps, n = _mx4(codes, scales, "the")
+    _check(ctx, load().som_update_mx4(ctx, pc, ps, n, _ptr(bmus, torch.int32, "bmus"),
+                                      _ptr(codebook, torch.float32, "codebook"), radius, scale))
+
+
+def som_train_epoch_mx4(ctx, codes, scales, codebook, radius: float, scale: float, bmus) -> None:
+    import torch
+    pc, ps, n = _mx4(codes, scales, "the")
+    _check(ctx, load().som_train_epoch_mx4(ctx, pc, ps, n, _ptr(codebook, torch.float32, "codebook"), radius, scale,
+                                           _ptr(bmus, torch.int32, "bmus")))
+
+
+def som_set_data_mx4(ctx, codes, scales) -> None:
+    pc, ps, n = _mx4(codes, scales, "the")
+    _check(ctx, load().som_set_data_mx4(ctx, pc, ps, n))
 
 
 def som_train(ctx, n_epochs: int, radius0: float, radiusN: float, scale0: float, scaleN: float, cooling: int,

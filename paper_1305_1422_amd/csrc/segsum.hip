@@ -15,6 +15,7 @@
 // chunking, with a column tile in LDS per chunk and atomic adds (k_accumulate_csr below): the order of
 // the additions is not fixed there, so two sparse runs agree to rounding only.
 #include "epoch_tables.hpp"
+#include "mx4.hpp"
 
 namespace som {
 
@@ -999,6 +1000,19 @@ hipError_t launch_scan_exclusive_i32(som_ctx *c, const int32_t *in, int32_t *out
 }
 
 // tables: where the epoch is in its schedule, if its tables are still to be written (then gather_pays(c, n) holds).
+// Sums of the chunks of every node (fp32 rows in c->partial) -> S.
+static hipError_t launch_combine(som_ctx *c, int64_t max_chunks) {
+  int ysplit = (c->dim + 255) / 256;
+  if (ysplit > 16) ysplit = 16;
+  const int cthreads = c->dim >= 256 ? 256 : (c->dim + 63) / 64 * 64;
+  if (max_chunks > kCombineGroup)
+    hipLaunchKernelGGL(k_combine_groups, dim3((unsigned)max_chunks, ysplit), dim3(cthreads), 0, c->stream, c->chunk_off,
+                       c->chunk_node, c->k, c->dim, c->partial);
+  hipLaunchKernelGGL(k_combine_chunks, dim3(c->k, ysplit), dim3(256), 0, c->stream, c->chunk_off, c->dim, c->partial,
+                     c->S);
+  return hipGetLastError();
+}
+
 hipError_t launch_accumulate_dense(som_ctx *c, const float *X, int64_t n, const int32_t *bmus, const EpochSchedule *tables) {
   if (gather_pays(c, n)) {
     int col_lanes = 16;
@@ -1027,15 +1041,68 @@ hipError_t launch_accumulate_dense(som_ctx *c, const float *X, int64_t n, const 
   else
     hipLaunchKernelGGL(k_accumulate_dense<false>, dim3((unsigned)max_chunks), dim3(threads), 0, c->stream, X,
                        c->dim, c->sort_val[0], c->seg_off, c->chunk_off, c->chunk_node, c->k, c->S, c->partial);
-  int ysplit = (c->dim + 255) / 256;
-  if (ysplit > 16) ysplit = 16;
-  const int cthreads = c->dim >= 256 ? 256 : (c->dim + 63) / 64 * 64;
-  if (max_chunks > kCombineGroup)
-    hipLaunchKernelGGL(k_combine_groups, dim3((unsigned)max_chunks, ysplit), dim3(cthreads), 0, c->stream, c->chunk_off,
-                       c->chunk_node, c->k, c->dim, c->partial);
-  hipLaunchKernelGGL(k_combine_chunks, dim3(c->k, ysplit), dim3(256), 0, c->stream, c->chunk_off, c->dim, c->partial,
-                     c->S);
-  return hipGetLastError();
+  return launch_combine(c, max_chunks);
+}
+
+// ---------------------------------------------------------------- microscaled 4-bit rows
+// A chunk's rows as in k_accumulate_dense, a word of eight elements per lane; the lanes that a row leaves over take further
+// rows of the chunk, and their sums are added in order.  A lane adds at most kChunkRows values of three significant bits in fp32, the lanes'
+// sums are added in fp64.
+__global__ __launch_bounds__(256) void k_accumulate_mx4(Mx4Rows x, int dim, int words /* of a row */, int cols /* lanes of a row */,
+                                                        const int32_t *__restrict__ perm, const int32_t *__restrict__ seg_off,
+                                                        const int32_t *__restrict__ chunk_off, const int32_t *__restrict__ chunk_node,
+                                                        int k, float *__restrict__ S, float *__restrict__ partial) {
+  __shared__ int s_rows[kChunkRows];
+  __shared__ float s_sum[256 * 8];
+  const int chunk = blockIdx.x;
+  if (chunk >= chunk_off[k]) return;
+  const int b = chunk_node[chunk];
+  const int first_chunk = chunk_off[b];
+  const int lo = seg_off[b] + (chunk - first_chunk) * kChunkRows;
+  const int hi = min(lo + kChunkRows, seg_off[b + 1]);
+  const int nrows = hi - lo;
+  if (threadIdx.x < nrows) s_rows[threadIdx.x] = perm[lo + threadIdx.x];
+  __syncthreads();
+  const bool single = (chunk_off[b + 1] - first_chunk) == 1;
+  float *dst = single ? S + (int64_t)b * dim : partial + (int64_t)chunk * dim;
+  const int col = threadIdx.x % cols, slot = threadIdx.x / cols, slots = 256 / cols;
+  for (int q0 = 0; q0 < words; q0 += cols) {
+    const int q = q0 + col;
+    float a[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (q < words)
+      for (int r = slot; r < nrows; r += slots) {
+        const int64_t row = s_rows[r];
+        const unsigned word = reinterpret_cast<const unsigned *>(x.codes)[row * words + q];
+        const float scale = mx4_scale(x.scales[row * (words / 4) + q / 4]);
+        const mx_f32x2 p0 = mx4_pair<0>(word, scale), p1 = mx4_pair<1>(word, scale), p2 = mx4_pair<2>(word, scale), p3 = mx4_pair<3>(word, scale);
+        a[0] += p0[0]; a[1] += p0[1]; a[2] += p1[0]; a[3] += p1[1]; a[4] += p2[0]; a[5] += p2[1]; a[6] += p3[0]; a[7] += p3[1];
+      }
+    if (q0) __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 8; ++u) s_sum[u * 256 + threadIdx.x] = a[u];
+    __syncthreads();
+    for (int t = threadIdx.x; t < 8 * cols; t += 256) {
+      const int u = t & 7, cc = t >> 3, c = (q0 + cc) * 8 + u;
+      if (c < dim) {
+        double sum = 0.0;
+        for (int s = 0; s < slots; ++s) sum += (double)s_sum[u * 256 + s * cols + cc];
+        dst[c] = (float)sum;
+      }
+    }
+  }
+}
+
+hipError_t launch_accumulate_mx4(som_ctx *c, Mx4Rows x, const int32_t *bmus) {
+  const hipError_t e = launch_group_by_bmu(c, bmus, x.n, kChunkRows);
+  if (e != hipSuccess) return e;
+  int64_t max_chunks = x.n / kChunkRows + (x.n < c->k ? x.n : c->k);
+  if (max_chunks < 1) max_chunks = 1;
+  const int words = 4 * mx4_blocks(c->dim);
+  int cols = 4;
+  while (cols < words && cols < 256) cols *= 2;
+  hipLaunchKernelGGL(k_accumulate_mx4, dim3((unsigned)max_chunks), dim3(256), 0, c->stream, x, c->dim, words, cols, c->sort_val[0],
+                     c->seg_off, c->chunk_off, c->chunk_node, c->k, c->S, c->partial);
+  return launch_combine(c, max_chunks);
 }
 
 hipError_t launch_accumulate_csr(som_ctx *c, const int64_t *indptr, const int32_t *indices,

@@ -801,6 +801,107 @@ static int registered_csr_dense(som_ctx *c) {
   return SOM_OK;
 }
 
+// ---------------------------------------------------------------- microscaled 4-bit rows
+// Scratch buffer `which` of at least `bytes`.  Its predecessor stays allocated (each is at least twice the one before), so that nothing has
+// to wait and what is recorded in a graph keeps its memory.  A call that is being recorded allocates nothing.
+static int mx4_scratch(som_ctx *c, int which, size_t bytes, void **out) {
+  if (bytes > c->mx4_cap[which]) {
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(c->stream, &capture) != hipSuccess || capture != hipStreamCaptureStatusNone) {
+      (void)hipGetLastError();
+      return fail(c, SOM_ERR_STATE, "a recorded call needs scratch: make a call of this size before recording");
+    }
+    const size_t cap = bytes > 2 * c->mx4_cap[which] ? bytes : 2 * c->mx4_cap[which];
+    Mx4Retired *old = c->mx4_buf[which] ? (Mx4Retired *)malloc(sizeof(Mx4Retired)) : nullptr;
+    char *buf = nullptr;
+    if ((c->mx4_buf[which] && !old) || !dev_alloc_first(c, &buf, cap)) {
+      (void)hipGetLastError();
+      free(old);
+      return fail(c, SOM_ERR_ALLOC, "cannot allocate %zu bytes of scratch for 4-bit rows", cap);
+    }
+    if (old) {
+      old->buf = c->mx4_buf[which];
+      old->next = c->mx4_retired;
+      c->mx4_retired = old;
+    }
+    c->mx4_buf[which] = buf;
+    c->mx4_cap[which] = cap;
+  }
+  *out = c->mx4_buf[which];
+  return SOM_OK;
+}
+
+static int check_mx4(som_ctx *c, const uint8_t *codes, const uint8_t *scales, int64_t n) {
+  if (!codes || !scales) return fail(c, SOM_ERR_INVALID_ARG, "codes or scales is NULL");
+  if ((uintptr_t)codes % 16 != 0) return fail(c, SOM_ERR_INVALID_ARG, "codes must be aligned to 16 bytes");
+  return check_rows(c, n);
+}
+
+// An array of rows of `width` elements of a type, `stride` elements apart.
+static int check_typed(som_ctx *c, const void *rows, int type, int64_t n, int64_t width, int64_t stride) {
+  if (!rows) return fail(c, SOM_ERR_INVALID_ARG, "NULL pointer argument");
+  if (type != SOM_FP32 && type != SOM_FP16 && type != SOM_BF16) return fail(c, SOM_ERR_INVALID_ARG, "unknown type %d", type);
+  if ((uintptr_t)rows % (type == SOM_FP32 ? 4 : 2) != 0) return fail(c, SOM_ERR_INVALID_ARG, "rows are not aligned to their type");
+  if (n > 1 && (stride < width || stride >= (1ll << 40))) return fail(c, SOM_ERR_INVALID_ARG, "row stride below the row's length or above 2^40");
+  return SOM_OK;
+}
+
+static int bmu_search_mx4(som_ctx *c, Mx4Rows x, Mx4Rows w, int32_t *bmus) {
+  void *scratch = nullptr;
+  const int rc = mx4_scratch(c, kMx4Search, mx4_search_bytes(c, x.n), &scratch);
+  if (rc) return rc;
+  c->two_level_n = 0;
+  c->sub_tried = 0;
+  StageTimer t(c, 0);
+  SOM_LAUNCH(c, launch_bmu_mx4(c, x, w, scratch, bmus));
+  return SOM_OK;
+}
+
+// Scratch of an epoch on n rows, for what is enqueued before its first launch to be complete.
+static int ensure_mx4_epoch(som_ctx *c, int64_t n) {
+  int rc = ensure_rows(c, n, true, false);
+  void *p = nullptr;
+  const size_t blocks = (size_t)mx4_blocks(c->dim);
+  if (!rc) rc = mx4_scratch(c, kMx4Search, mx4_search_bytes(c, n), &p);
+  if (!rc) rc = mx4_scratch(c, kMx4Codes, (size_t)c->k * blocks * 16, &p);
+  if (!rc) rc = mx4_scratch(c, kMx4Scales, (size_t)c->k * blocks, &p);
+  return rc;
+}
+
+static int update_mx4(som_ctx *c, Mx4Rows x, const int32_t *bmus, float *W) {
+  {
+    StageTimer t(c, 3);
+    SOM_LAUNCH(c, launch_accumulate_mx4(c, x, bmus));
+  }
+  StageTimer t(c, 4);
+  SOM_LAUNCH(c, launch_smooth_and_divide(c, W));
+  return SOM_OK;
+}
+
+// The search of an epoch goes through the code book in the rows' own form.
+static int epoch_mx4(som_ctx *c, Mx4Rows x, float *W, int32_t *bmus) {
+  const Mx4Rows w = {static_cast<uint8_t *>(c->mx4_buf[kMx4Codes]), static_cast<uint8_t *>(c->mx4_buf[kMx4Scales]), c->k};
+  {
+    StageTimer t(c, 5);
+    SOM_LAUNCH(c, launch_mx4_quantize(c->stream, W, SOM_FP32, c->k, c->dim, c->dim, static_cast<uint8_t *>(c->mx4_buf[kMx4Codes]),
+                                      static_cast<uint8_t *>(c->mx4_buf[kMx4Scales])));
+  }
+  const int rc = bmu_search_mx4(c, x, w, bmus);
+  return rc ? rc : update_mx4(c, x, bmus, W);
+}
+
+// Nothing is registered, and nothing that was computed of a registered set holds.
+static void forget_registered(som_ctx *c) {
+  c->data_kind = 0; c->d_data = nullptr; c->d_n = 0; c->d_nnz = 0;
+  c->d_indptr = nullptr; c->d_indices = nullptr; c->d_values = nullptr;
+  c->d_norms_valid = 0;
+  c->d_split_valid = 0;
+  c->hot_valid = 0;
+  c->hot_on = 0;
+  c->csrd_valid = 0;
+  c->csrd_on = 0;
+}
+
 static bool is_registered_dense(const som_ctx *c, const float *data, int64_t n) {
   return c->data_kind == 1 && data == c->d_data && n == c->d_n;
 }
@@ -912,6 +1013,13 @@ void som_destroy(som_ctx *c) {
   dev_free(c->csrd_mu); dev_free(c->csrd_mu_norm2); dev_free(c->csrd_xn);
   dev_free(c->hot_counts); dev_free(c->hot_rank); dev_free(c->hot_cols); dev_free(c->hot_Wc); dev_free(c->hot_Wh);
   dev_free(c->hot_wscale);
+  for (int b = 0; b < kMx4Bufs; ++b) dev_free(c->mx4_buf[b]);
+  while (c->mx4_retired) {
+    Mx4Retired *r = c->mx4_retired;
+    c->mx4_retired = r->next;
+    dev_free(r->buf);
+    free(r);
+  }
   for (int s = 0; s < SOM_PROFILE_STAGES; ++s) {
     if (!c->prof_ev[s]) continue;
     for (int e = 0; e < 2 * kProfMax; ++e) (void)hipEventDestroy(c->prof_ev[s][e]);
@@ -1053,6 +1161,80 @@ int som_train_epoch_csr(som_ctx *c, const int64_t *indptr, const int32_t *indice
   return update_csr(c, indptr, indices, values, n, nnz, bmus, codebook);
 }
 
+int som_mx4_quantize(som_ctx *c, const void *rows, int type, int64_t n, int64_t stride, uint8_t *codes, uint8_t *scales) {
+  if (!c) return SOM_ERR_INVALID_ARG;
+  int rc = check_mx4(c, codes, scales, n);
+  if (!rc) rc = check_typed(c, rows, type, n, c->dim, stride);
+  if (rc) return rc;
+  SOM_LAUNCH(c, launch_mx4_quantize(c->stream, rows, type, n, stride, c->dim, codes, scales));
+  return SOM_OK;
+}
+
+int som_mx4_dequantize(som_ctx *c, const uint8_t *codes, const uint8_t *scales, int64_t n, void *rows, int type, int64_t stride) {
+  if (!c) return SOM_ERR_INVALID_ARG;
+  int rc = check_mx4(c, codes, scales, n);
+  if (!rc) rc = check_typed(c, rows, type, n, c->dim, stride);
+  if (rc) return rc;
+  SOM_LAUNCH(c, launch_mx4_dequantize(c->stream, Mx4Rows{codes, scales, n}, c->dim, rows, type, stride));
+  return SOM_OK;
+}
+
+int som_mx4_product(som_ctx *c, const uint8_t *codes_a, const uint8_t *scales_a, int64_t n, const uint8_t *codes_b,
+                    const uint8_t *scales_b, int64_t m, void *out, int type, int64_t stride) {
+  if (!c) return SOM_ERR_INVALID_ARG;
+  int rc = check_mx4(c, codes_a, scales_a, n);
+  if (!rc) rc = check_mx4(c, codes_b, scales_b, m);
+  if (!rc) rc = check_typed(c, out, type, n, m, stride);
+  if (rc) return rc;
+  SOM_LAUNCH(c, launch_mx4_product(c, Mx4Rows{codes_a, scales_a, n}, Mx4Rows{codes_b, scales_b, m}, out, type, stride));
+  return SOM_OK;
+}
+
+int som_bmus_mx4(som_ctx *c, const uint8_t *codes, const uint8_t *scales, int64_t n, const uint8_t *node_codes,
+                 const uint8_t *node_scales, int32_t *bmus) {
+  if (!c) return SOM_ERR_INVALID_ARG;
+  int rc = check_mx4(c, codes, scales, n);
+  if (!rc) rc = check_mx4(c, node_codes, node_scales, c->k);
+  if (!rc && !bmus) rc = fail(c, SOM_ERR_INVALID_ARG, "NULL pointer argument");
+  if (rc) return rc;
+  return bmu_search_mx4(c, Mx4Rows{codes, scales, n}, Mx4Rows{node_codes, node_scales, c->k}, bmus);
+}
+
+int som_update_mx4(som_ctx *c, const uint8_t *codes, const uint8_t *scales, int64_t n, const int32_t *bmus, float *codebook,
+                   float radius, float scale) {
+  if (!c) return SOM_ERR_INVALID_ARG;
+  if (!codebook || !bmus) return fail(c, SOM_ERR_INVALID_ARG, "NULL pointer argument");
+  int rc = check_mx4(c, codes, scales, n);
+  if (!rc) rc = check_epoch_scalars(c, radius, scale);
+  if (!rc) rc = ensure_rows(c, n, true, false);
+  if (rc) return rc;
+  SOM_LAUNCH(c, launch_epoch_params(c, epoch_schedule(c, 0, 1, radius, radius, scale, scale, SOM_COOL_LINEAR), false));
+  return update_mx4(c, Mx4Rows{codes, scales, n}, bmus, codebook);
+}
+
+int som_train_epoch_mx4(som_ctx *c, const uint8_t *codes, const uint8_t *scales, int64_t n, float *codebook, float radius,
+                        float scale, int32_t *bmus) {
+  if (!c) return SOM_ERR_INVALID_ARG;
+  if (!codebook || !bmus) return fail(c, SOM_ERR_INVALID_ARG, "NULL pointer argument");
+  int rc = check_mx4(c, codes, scales, n);
+  if (!rc) rc = check_epoch_scalars(c, radius, scale);
+  if (!rc) rc = ensure_mx4_epoch(c, n);
+  if (rc) return rc;
+  SOM_LAUNCH(c, launch_epoch_params(c, epoch_schedule(c, 0, 1, radius, radius, scale, scale, SOM_COOL_LINEAR), false));
+  return epoch_mx4(c, Mx4Rows{codes, scales, n}, codebook, bmus);
+}
+
+int som_set_data_mx4(som_ctx *c, const uint8_t *codes, const uint8_t *scales, int64_t n) {
+  if (!c) return SOM_ERR_INVALID_ARG;
+  const int rc = check_mx4(c, codes, scales, n);
+  if (rc) return rc;
+  forget_registered(c);
+  c->data_kind = 3;
+  c->d_n = n;
+  c->d_mx4 = Mx4Rows{codes, scales, n};
+  return SOM_OK;
+}
+
 int som_set_data_dense(som_ctx *c, const float *data, int64_t n) {
   if (!c) return SOM_ERR_INVALID_ARG;
   if (!data) return fail(c, SOM_ERR_INVALID_ARG, "data is NULL");
@@ -1116,18 +1298,20 @@ int som_train_snapshots(som_ctx *c, int n_epochs, float radius0, float radiusN, 
   schedule_defaults(c, radius0, radiusN, scale0, scaleN);
   if (!isfinite(radius0) || !isfinite(radiusN)) return fail(c, SOM_ERR_INVALID_ARG, "radius not finite");
   if (scale0 > 1.f || scaleN > 1.f) return fail(c, SOM_ERR_INVALID_ARG, "scale must be in (0, 1]");
-  const bool dense = c->data_kind == 1;
-  const bool direct = dense && direct_search(c, c->d_n, true);
-  int rc = ensure_rows(c, c->d_n, dense, !direct);
+  const bool dense = c->data_kind == 1, mx4 = c->data_kind == 3;
+  const bool direct = mx4 || (dense && direct_search(c, c->d_n, true));
+  int rc = mx4 ? ensure_mx4_epoch(c, c->d_n) : ensure_rows(c, c->d_n, dense, !direct);
   if (!rc && !direct) rc = registered_norms(c);
-  if (!rc && !dense) rc = registered_csr_dense(c);
-  if (!rc && !dense && !c->csrd_on) rc = registered_hot(c);
+  if (!rc && !dense && !mx4) rc = registered_csr_dense(c);
+  if (!rc && !dense && !mx4 && !c->csrd_on) rc = registered_hot(c);
   if (rc) return rc;
   for (int e = 0; e < n_epochs; ++e) {
     const EpochSchedule q = epoch_schedule(c, e, n_epochs, radius0, radiusN, scale0, scaleN, cooling);
     const EpochSchedule *later = dense ? tables_later(c, c->d_n, !direct, q) : nullptr;
     if (!later) SOM_LAUNCH(c, launch_epoch_params(c, q, !direct));
-    if (dense) {
+    if (mx4) {
+      rc = epoch_mx4(c, c->d_mx4, codebook, bmus);
+    } else if (dense) {
       rc = direct ? bmu_search_direct(c, c->d_data, c->d_n, codebook, bmus)
                   : bmu_search_dense(c, c->d_data, c->d_n, codebook, bmus, true, true,
                                      e > 0 ? cooled(radius0, radiusN, n_epochs, e, cooling) : 0.0 /* the first code book is the caller's */);

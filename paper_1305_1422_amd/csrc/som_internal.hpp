@@ -124,6 +124,20 @@ struct EpochParams {
 }  // namespace som
 
 // ---------------------------------------------------------------- context
+namespace som {
+// Microscaled 4-bit rows in device memory (mx4.hpp): codes [n][16 B], scales [n][B], B = mx4_blocks(dim).
+struct Mx4Rows {
+  const uint8_t *codes, *scales;
+  int64_t n;
+};
+inline int mx4_blocks(int dim) { return (dim + 31) / 32; }
+enum { kMx4Search = 0, kMx4Codes = 1, kMx4Scales = 2, kMx4Bufs = 3 };
+struct Mx4Retired {
+  void *buf;
+  Mx4Retired *next;
+};
+}  // namespace som
+
 struct som_ctx {
   int rows, cols, dim, k;
   int map_type, grid_type;
@@ -278,8 +292,15 @@ struct som_ctx {
   float *csrd_xn;         // [n] squared norms of the centred rows
   int64_t csrd_n_cap;
 
+  // scratch of the calls on microscaled 4-bit rows (som_api.hip: mx4_scratch); a buffer that has become too small is kept until
+  // som_destroy, because work enqueued or recorded earlier may still use it
+  void *mx4_buf[som::kMx4Bufs];
+  size_t mx4_cap[som::kMx4Bufs];
+  som::Mx4Retired *mx4_retired;
+
   // registered training set for som_train
-  int data_kind;          // 0 none, 1 dense, 2 csr
+  int data_kind;          // 0 none, 1 dense, 2 csr, 3 microscaled 4-bit
+  som::Mx4Rows d_mx4;
   const float *d_data;
   const int64_t *d_indptr;
   const int32_t *d_indices;
@@ -458,6 +479,18 @@ hipError_t launch_accumulate_dense(som_ctx *c, const float *X, int64_t n, const 
                                    const EpochSchedule *tables);               // -> S, counts (... and writes the epoch's tables if asked)
 hipError_t launch_accumulate_csr(som_ctx *c, const int64_t *indptr, const int32_t *indices,
                                  const float *values, int64_t n, int64_t nnz, const int32_t *bmus);   // -> S, counts
+
+hipError_t launch_accumulate_mx4(som_ctx *c, Mx4Rows x, const int32_t *bmus);                          // -> S, counts
+
+// mx4.hip: type SOM_FP32, SOM_FP16 or SOM_BF16, stride in elements
+hipError_t launch_mx4_quantize(hipStream_t stream, const void *rows, int type, int64_t n, int64_t stride, int dim, uint8_t *codes,
+                               uint8_t *scales);
+hipError_t launch_mx4_dequantize(hipStream_t stream, Mx4Rows x, int dim, void *rows, int type, int64_t stride);
+// mx4_product.hip
+hipError_t launch_mx4_product(som_ctx *c, Mx4Rows a, Mx4Rows b, void *out, int type, int64_t stride);
+// bmu_mx4.hip
+size_t mx4_search_bytes(const som_ctx *c, int64_t n);       // scratch of a search of n rows among the c->k nodes
+hipError_t launch_bmu_mx4(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int32_t *bmus);
 
 // smooth.hip
 hipError_t launch_epoch_params(som_ctx *c, const EpochSchedule &q, bool search);

@@ -2,7 +2,7 @@
 output buffers as torch tensors on the GPU.  No arithmetic happens here."""
 from __future__ import annotations
 
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -16,8 +16,20 @@ FILTERS = {"fp32": capi.SOM_FILTER_FP32, "split_f16": capi.SOM_FILTER_SPLIT_F16,
 NEIGHBORHOODS = {"gaussian": capi.SOM_NEIGHBORHOOD_GAUSSIAN, "bubble": capi.SOM_NEIGHBORHOOD_BUBBLE}
 
 
+class Mx4(NamedTuple):
+    """Rows in microscaled 4-bit form: ``codes`` uint8 [n, 16 B], ``scales`` uint8 [n, B], B = ceil(dim / 32) (the
+    format is described at som_mx4_quantize in include/som.h).  Made by ``Som.quantize_mx4``."""
+
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+
+def _is_mx4(data) -> bool:
+    return isinstance(data, Mx4)
+
+
 def _is_csr(data) -> bool:
-    return isinstance(data, (tuple, list)) and len(data) == 3
+    return not _is_mx4(data) and isinstance(data, (tuple, list)) and len(data) == 3
 
 
 class Som:
@@ -26,7 +38,7 @@ class Som:
     ``codebook``: optional float32 tensor [rows*cols, dim] (copied to the device) - the
     initial code book; otherwise ``seed`` (non-zero) draws a uniform [0,1) one on the device.
     Dense data: float32 tensor [n, dim].  Sparse data: tuple (indptr int64 [n+1], indices
-    int32 [nnz], values float32 [nnz]).
+    int32 [nnz], values float32 [nnz]).  Microscaled 4-bit data: ``Mx4``.
     """
 
     default_filter: Optional[str] = None     # None = the library's default; tests switch it
@@ -99,41 +111,111 @@ class Som:
             pass
 
     def _n(self, data) -> int:
-        return (data[0].shape[0] - 1) if _is_csr(data) else data.shape[0]
+        return data.codes.shape[0] if _is_mx4(data) else (data[0].shape[0] - 1) if _is_csr(data) else data.shape[0]
+
+    def _check_mx4(self, data: Mx4, rows: Optional[int] = None) -> None:
+        """Refuses what is not rows of this map's features."""
+        if not _is_mx4(data):
+            raise TypeError("expected microscaled 4-bit rows (Mx4)")
+        n, blocks = data.scales.shape
+        if blocks != (self.dim + 31) // 32:
+            raise ValueError(f"rows of {blocks} blocks of 32 do not fit {self.dim} features")
+        if rows is not None and n != rows:
+            raise ValueError(f"expected {rows} rows, got {n}")
+
+    def _check_bmus(self, data, bmus: torch.Tensor) -> None:
+        if bmus.numel() < self._n(data):
+            raise ValueError("bmus is shorter than the data")
+
+    def quantize_mx4(self, rows: torch.Tensor, out: Optional[Mx4] = None) -> Mx4:
+        """Rows [n, dim] of float32, float16 or bfloat16 (they may lie apart) in microscaled 4-bit form."""
+        if rows.dim() != 2 or rows.shape[1] != self.dim:
+            raise ValueError(f"expected rows of {self.dim} features")
+        n, blocks = rows.shape[0], (self.dim + 31) // 32
+        if out is None:
+            out = Mx4(torch.empty((n, 16 * blocks), dtype=torch.uint8, device=self.device),
+                      torch.empty((n, blocks), dtype=torch.uint8, device=self.device))
+        capi.som_mx4_quantize(self.ctx, rows, out.codes, out.scales)
+        return out
+
+    def dequantize_mx4(self, data: Mx4, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The values that rows in microscaled 4-bit form stand for, [n, dim]."""
+        self._check_mx4(data)
+        if out is None:
+            out = torch.empty((data.codes.shape[0], self.dim), dtype=dtype, device=self.device)
+        elif out.dim() != 2 or out.shape[1] != self.dim:
+            raise ValueError(f"expected room for rows of {self.dim} features")
+        capi.som_mx4_dequantize(self.ctx, data.codes, data.scales, out)
+        return out
+
+    def products_mx4(self, a: Mx4, b: Mx4, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Dot products of all rows of a with all rows of b, [n, m]."""
+        self._check_mx4(a)
+        self._check_mx4(b)
+        if out is None:
+            out = torch.empty((a.codes.shape[0], b.codes.shape[0]), dtype=dtype, device=self.device)
+        capi.som_mx4_product(self.ctx, a.codes, a.scales, b.codes, b.scales, out)
+        return out
 
     def _new_bmus(self, data) -> torch.Tensor:
         return torch.empty(self._n(data), dtype=torch.int32, device=self.device)
 
     def train_epoch(self, data, radius: float, scale: float = 1.0, bmus: Optional[torch.Tensor] = None):
         bmus = self._new_bmus(data) if bmus is None else bmus
-        if _is_csr(data):
+        if _is_mx4(data):
+            self._check_mx4(data)
+            self._check_bmus(data, bmus)
+            capi.som_train_epoch_mx4(self.ctx, data.codes, data.scales, self.codebook, radius, scale, bmus)
+        elif _is_csr(data):
             capi.som_train_epoch_csr(self.ctx, data[0], data[1], data[2], self.codebook, radius, scale, bmus)
         else:
             capi.som_train_epoch_dense(self.ctx, data, self.codebook, radius, scale, bmus)
         return bmus
 
-    def bmus(self, data, bmus: Optional[torch.Tensor] = None):
+    def bmus(self, data, bmus: Optional[torch.Tensor] = None, nodes: Optional[Mx4] = None):
+        """Nearest node of every instance.  Microscaled 4-bit data are compared with ``nodes``, the code book in the
+        same form (``quantize_mx4``); without it the code book is brought into that form by the call."""
         bmus = self._new_bmus(data) if bmus is None else bmus
-        if _is_csr(data):
+        if nodes is not None and not _is_mx4(data):
+            raise TypeError("nodes belongs to microscaled 4-bit data")
+        if _is_mx4(data):
+            if nodes is None:
+                with torch.cuda.stream(self.stream):      # theirs to free: nothing else may get their memory before the search is done
+                    nodes = self.quantize_mx4(self.codebook)
+            self._check_mx4(data)
+            self._check_mx4(nodes, self.k)
+            self._check_bmus(data, bmus)
+            capi.som_bmus_mx4(self.ctx, data.codes, data.scales, nodes.codes, nodes.scales, bmus)
+        elif _is_csr(data):
             capi.som_bmus_csr(self.ctx, data[0], data[1], data[2], self.codebook, bmus)
         else:
             capi.som_bmus_dense(self.ctx, data, self.codebook, bmus)
         return bmus
 
     def update(self, data, bmus: torch.Tensor, radius: float, scale: float = 1.0) -> None:
-        if _is_csr(data):
+        if _is_mx4(data):
+            self._check_mx4(data)
+            self._check_bmus(data, bmus)
+            capi.som_update_mx4(self.ctx, data.codes, data.scales, bmus, self.codebook, radius, scale)
+        elif _is_csr(data):
             capi.som_update_csr(self.ctx, data[0], data[1], data[2], bmus, self.codebook, radius, scale)
         else:
             capi.som_update_dense(self.ctx, data, bmus, self.codebook, radius, scale)
 
-    def train(self, data, n_epochs: int, radius0: float = 0.0, radiusN: float = 0.0, scale0: float = 0.0,
-              scaleN: float = 0.0, cooling: str = "linear", bmus: Optional[torch.Tensor] = None):
-        bmus = self._new_bmus(data) if bmus is None else bmus
-        if _is_csr(data):
+    def _register(self, data) -> None:
+        if _is_mx4(data):
+            self._check_mx4(data)
+            capi.som_set_data_mx4(self.ctx, data.codes, data.scales)
+        elif _is_csr(data):
             capi.som_set_data_csr(self.ctx, data[0], data[1], data[2])
         else:
             capi.som_set_data_dense(self.ctx, data)
         self._data = data        # keep the registered tensors alive
+
+    def train(self, data, n_epochs: int, radius0: float = 0.0, radiusN: float = 0.0, scale0: float = 0.0,
+              scaleN: float = 0.0, cooling: str = "linear", bmus: Optional[torch.Tensor] = None):
+        bmus = self._new_bmus(data) if bmus is None else bmus
+        self._register(data)
         capi.som_train(self.ctx, n_epochs, radius0, radiusN, scale0, scaleN, COOLING[cooling], self.codebook, bmus)
         return bmus
 
@@ -141,11 +223,7 @@ class Som:
                         scale0: float = 0.0, scaleN: float = 0.0, cooling: str = "linear"):
         """train() with the interim outputs of option -s: returns (bmus, umatrices[, codebooks, bmus_all])."""
         bmus = self._new_bmus(data)
-        if _is_csr(data):
-            capi.som_set_data_csr(self.ctx, data[0], data[1], data[2])
-        else:
-            capi.som_set_data_dense(self.ctx, data)
-        self._data = data
+        self._register(data)
         n = bmus.shape[0]
         um = torch.empty((n_epochs, self.rows, self.cols), dtype=torch.float32, device=self.device) \
             if snapshots >= 1 else None

@@ -1,0 +1,538 @@
+"""Microscaled 4-bit rows against their definition in fp64: form and back, products, searches, updates, epochs and schedules."""
+import numpy as np
+import pytest
+
+from tests import mx4_reference as R
+from tests import parity as P
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+TYPES = {"fp32": torch.float32, "fp16": torch.float16, "bf16": torch.bfloat16}
+HALF_STEP = {"fp32": 2.0 ** -24, "fp16": 2.0 ** -11, "bf16": 2.0 ** -8}
+DIMS = [1, 7, 31, 32, 33, 64, 96, 100, 128, 130, 1000]
+
+
+def make(rows=1, cols=1, dim=32, codebook=None, **kw):
+    from paper_1305_1422_amd import Som
+    cb = np.zeros((rows * cols, dim), np.float32) if codebook is None else codebook
+    return Som(rows, cols, dim, codebook=torch.from_numpy(np.ascontiguousarray(cb)), **kw)
+
+
+def dev(stored):
+    from paper_1305_1422_amd import Mx4
+    return Mx4(P.to_dev(stored[0]), P.to_dev(stored[1]))
+
+
+def host(mx):
+    return mx.codes.cpu().numpy(), mx.scales.cpu().numpy()
+
+
+# ---------------------------------------------------------------- form and back
+def awkward_rows(rng, n, dim):
+    """Blocks of every size of element, halfway values, zeros of both signs, subnormal, huge and non-finite ones."""
+    x = rng.standard_normal((n, dim)) * np.exp2(rng.integers(-20, 20, (n, dim)) * (rng.random((n, 1)) < 0.5))
+    kind = rng.integers(0, 8, n)
+    x[kind == 0] = np.round(x[kind == 0] * 4) / 4
+    x[kind == 1] = 0.0
+    x[kind == 2] *= 2.0 ** -130
+    x[kind == 3] *= 2.0 ** 90
+    x[rng.random((n, dim)) < 0.02] = -0.0
+    return x
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("dim", DIMS)
+def test_quantize(kind, dim):
+    rng = np.random.default_rng(100 + dim)
+    n = 301
+    x = awkward_rows(rng, n, dim)
+    with np.errstate(over="ignore"):
+        t = torch.from_numpy(x.astype(np.float32)).to(TYPES[kind])
+    if dim > 1:
+        t[5, dim // 2], t[6, 0], t[7, dim - 1] = float("inf"), float("nan"), -float("inf")
+    want = R.quantize(t.double().numpy())
+    som = make(dim=dim)
+    got = host(som.quantize_mx4(t.cuda()))
+    assert np.array_equal(got[1], want[1])
+    assert np.array_equal(got[0], want[0])
+    som.close()
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("dim,stride,offset", [(64, 64, 0), (64, 72, 0), (64, 65, 0), (64, 72, 1), (33, 40, 3), (8, 9, 0), (100, 104, 4)])
+def test_rows_that_lie_apart(kind, dim, stride, offset):
+    """Row strides and bases that allow 16-byte accesses and that do not; what lies between the rows is left as it is."""
+    rng = np.random.default_rng(stride)
+    n = 77
+    wide = torch.from_numpy(rng.standard_normal(offset + n * stride).astype(np.float32)).to(TYPES[kind]).cuda()
+    rows = torch.as_strided(wide, (n, dim), (stride, 1), offset)
+    som = make(dim=dim)
+    mx = som.quantize_mx4(rows)
+    want = R.quantize(rows.double().cpu().numpy())
+    assert np.array_equal(host(mx)[0], want[0]) and np.array_equal(host(mx)[1], want[1])
+    before = wide.clone()
+    som.dequantize_mx4(mx, out=rows)
+    keep = torch.ones_like(wide, dtype=torch.bool)
+    torch.as_strided(keep, (n, dim), (stride, 1), offset).fill_(False)
+    assert torch.equal(wide[keep], before[keep])
+    assert np.array_equal(rows.double().cpu().numpy(), R.values(*want, dim))
+    som.close()
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_dequantize_every_code_and_scale(kind):
+    codes = np.tile(np.arange(256, dtype=np.uint8).reshape(1, 256), (256, 1))
+    scales = np.tile(np.arange(256, dtype=np.uint8).reshape(256, 1), (1, 16))
+    want = torch.from_numpy(R.values(codes, scales, 512)).to(torch.float32).to(TYPES[kind])      # exact, then one rounding
+    som = make(dim=512)
+    got = som.dequantize_mx4(dev((codes, scales)), TYPES[kind]).cpu()
+    nan = torch.isnan(want)
+    assert torch.equal(torch.isnan(got), nan) and torch.equal(got[~nan], want[~nan])
+    assert torch.equal(torch.signbit(got[~nan]), torch.signbit(want[~nan]))
+    som.close()
+
+
+@pytest.mark.parametrize("n", [1, 2, 63, 4097])
+def test_round_trip_of_few_and_many_rows(n):
+    rng = np.random.default_rng(n)
+    x = rng.standard_normal((n, 45)).astype(np.float32)
+    som = make(dim=45)
+    got = som.dequantize_mx4(som.quantize_mx4(P.to_dev(x))).cpu().numpy()
+    assert np.array_equal(got, R.values(*R.quantize(x), 45))
+    som.close()
+
+
+# ---------------------------------------------------------------- products
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("n,m,dim", [(1, 1, 1), (1, 70, 33), (3, 17, 128), (65, 63, 129), (64, 64, 32), (130, 300, 100), (257, 259, 512),
+                                     (300, 70, 1000), (40, 513, 1500), (16, 16, 4096)])
+def test_product(kind, n, m, dim):
+    """The instruction's four block sums and its addend are cut off at 2^-20 of their magnitudes at most, once for every 128
+    features, then there is one rounding to the type."""
+    rng = np.random.default_rng(n + m + dim)
+    a, b = R.random_rows(rng, n, dim), R.random_rows(rng, m, dim)
+    som = make(dim=dim)
+    got = som.products_mx4(dev(a), dev(b), TYPES[kind]).double().cpu().numpy()
+    va, vb = R.values(*a, dim), R.values(*b, dim)
+    want, size = va @ vb.T, np.abs(va) @ np.abs(vb).T
+    tol = (dim + 127) // 128 * 2.0 ** -20 * size
+    tol = tol + HALF_STEP[kind] * (np.abs(want) + tol)
+    over = np.abs(want) > 65504 * (1 + 2.0 ** -11) if kind == "fp16" else np.zeros_like(want, bool)
+    assert np.all((np.abs(got - want) <= tol) | over)
+    som.close()
+
+
+def test_product_is_exact_where_scales_are_alike():
+    """Products of one scale are multiples of one number, and their sums stay below 2^24 of it."""
+    rng = np.random.default_rng(3)
+    a, b = R.random_rows(rng, 70, 1000, 127, 127), R.random_rows(rng, 90, 1000, 120, 120)
+    som = make(dim=1000)
+    got = som.products_mx4(dev(a), dev(b)).double().cpu().numpy()
+    assert np.array_equal(got, R.values(*a, 1000) @ R.values(*b, 1000).T)
+    som.close()
+
+
+def test_product_of_not_a_number_and_extremes():
+    rng = np.random.default_rng(4)
+    a, b = R.random_rows(rng, 20, 200), R.random_rows(rng, 30, 200)
+    a[1][3, 2], b[1][7, 6] = 255, 255
+    a[1][4, :], a[1][5, :] = 254, 0
+    som = make(dim=200)
+    got = som.products_mx4(dev(a), dev(b)).double().cpu().numpy()
+    assert np.isnan(got[3]).all() and np.isnan(got[:, 7]).all()
+    with np.errstate(over="ignore", invalid="ignore"):
+        want = R.values(*a, 200) @ R.values(*b, 200).T
+        size = np.abs(R.values(*a, 200)) @ np.abs(R.values(*b, 200)).T
+    rest = np.ones((20, 30), bool)
+    rest[3], rest[:, 7], rest[4] = False, False, False
+    assert np.all(np.abs(got - want)[rest] <= (2 * 2.0 ** -20 * size + 2.0 ** -24 * np.abs(want) + 2.0 ** -120)[rest])
+    assert not np.isfinite(got[4][np.abs(want[4]) > 2.0 ** 129]).any()
+    som.close()
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_product_into_rows_that_lie_apart(kind):
+    rng = np.random.default_rng(5)
+    a, b = R.random_rows(rng, 37, 64, 127, 127), R.random_rows(rng, 41, 64, 127, 127)
+    som = make(dim=64)
+    for stride, offset in ((41, 0), (47, 0), (48, 0), (48, 3)):
+        wide = torch.full((offset + 37 * stride,), 7.0, dtype=TYPES[kind], device="cuda")
+        out = torch.as_strided(wide, (37, 41), (stride, 1), offset)
+        som.products_mx4(dev(a), dev(b), out=out)
+        want = torch.from_numpy(R.values(*a, 64) @ R.values(*b, 64).T).to(TYPES[kind])
+        assert torch.equal(out.cpu(), want)
+        keep = torch.ones_like(wide, dtype=torch.bool)
+        torch.as_strided(keep, (37, 41), (stride, 1), offset).fill_(False)
+        assert (wide[keep] == 7.0).all()
+    som.close()
+
+
+# ---------------------------------------------------------------- searches
+def search(som, x, w):
+    return som.bmus(dev(x), nodes=dev(w)).cpu().numpy()
+
+
+def check_search(x, w, dim, rows=1):
+    k = w[1].shape[0]
+    som = make(rows, k // rows, dim)
+    got = search(som, x, w)
+    som.close()
+    want = R.nearest(R.values(*x, dim), R.values(*w, dim))
+    bad = np.nonzero(got != want)[0]
+    assert bad.size == 0, f"{bad.size} of {got.size} differ, first {bad[0]}: {got[bad[0]]} for {want[bad[0]]}"
+
+
+SIZES = [(1, 1, 1), (1, 3, 40), (5, 64, 32), (17, 65, 33), (64, 16, 128), (100, 400, 10), (65, 130, 129), (300, 77, 1000), (1000, 1025, 100),
+         (1, 2500, 1000), (3, 5000, 96), (2000, 63, 257), (4099, 640, 128), (513, 2000, 1024), (700, 900, 1100), (130, 300, 4096)]
+
+
+@pytest.mark.parametrize("n,k,dim", SIZES)
+def test_search(n, k, dim):
+    rng = np.random.default_rng(n + k + dim)
+    check_search(R.quantize(rng.standard_normal((n, dim))), R.quantize(rng.standard_normal((k, dim))), dim)
+
+
+@pytest.mark.parametrize("n,k,dim", [(3, 70, 32), (1500, 700, 96), (600, 400, 1030)])
+def test_search_among_copies(n, k, dim):
+    """Ties: few distinct nodes, each many times; the lowest index of the nearest ones."""
+    rng = np.random.default_rng(n)
+    few = rng.standard_normal((5, dim))
+    w = R.quantize(few[rng.integers(0, 5, k)])
+    check_search(R.quantize(rng.standard_normal((n, dim))), w, dim)
+
+
+@pytest.mark.parametrize("n,k,dim", [(2, 100, 64), (2000, 1000, 64), (300, 300, 1200)])
+def test_search_on_a_coarse_grid(n, k, dim):
+    """Small whole numbers: many nodes are equally near."""
+    rng = np.random.default_rng(k)
+    x, w = rng.integers(-1, 2, (n, dim)).astype(float), rng.integers(-1, 2, (k, dim)).astype(float)
+    x[:, 5:] = 0.0
+    w[:, 5:] = 0.0
+    x[:, 0], w[:, 0] = 1.0, 1.0
+    check_search(R.quantize(x), R.quantize(w), dim)
+
+
+@pytest.mark.parametrize("n", [2, 1200])
+def test_search_among_near_copies(n):
+    """Nodes that differ in one small block: their scores differ by less than fp32 keeps of their sums."""
+    rng = np.random.default_rng(11)
+    dim, k = 160, 500
+    base = rng.standard_normal((4, dim)) * 64
+    w = base[rng.integers(0, 4, k)].copy()
+    w[:, 128:] = rng.standard_normal((k, 32)) * 2.0 ** -9
+    x = base[rng.integers(0, 4, n)].copy()
+    x[:, 128:] = rng.standard_normal((n, 32)) * 2.0 ** -9
+    check_search(R.quantize(x), R.quantize(w), dim)
+
+
+@pytest.mark.parametrize("n", [4, 900])
+@pytest.mark.parametrize("low,high", [(107, 147), (1, 20), (230, 250), (60, 75)])
+def test_search_over_wide_scales(n, low, high):
+    """Scales far from one another, sums that underflow or overflow fp32; within a node's and instance's 2^40 (fp64 exact)."""
+    rng = np.random.default_rng(low)
+    dim, k = 96, 333
+    span = min(10, high - low)
+    x, w = R.random_rows(rng, n, dim, 0, 0), R.random_rows(rng, k, dim, 0, 0)
+    x[1][:] = low + rng.integers(0, span, x[1].shape)
+    w[1][:] = low + rng.integers(0, span, w[1].shape)
+    w[1][::7] = (high - span) + rng.integers(0, span, w[1][::7].shape) if high - low <= 20 else w[1][::7]
+    check_search(x, w, dim)
+
+
+@pytest.mark.parametrize("n,k", [(4, 40), (700, 400)])
+def test_search_with_not_a_number(n, k):
+    rng = np.random.default_rng(13)
+    dim = 100
+    x, w = R.random_rows(rng, n, dim), R.random_rows(rng, k, dim)
+    w[1][::3, 1] = 255
+    w[1][0, :] = 255
+    x[1][1::5, 2] = 255
+    check_search(x, w, dim)
+    w[1][:, 0] = 255                            # no node at all: node 0
+    check_search(x, w, dim)
+
+
+@pytest.mark.parametrize("n", [1, 500])
+def test_search_of_zeros(n):
+    dim, k = 64, 200
+    rng = np.random.default_rng(14)
+    zero = R.quantize(np.zeros((n, dim)))
+    check_search(zero, R.quantize(rng.standard_normal((k, dim))), dim)
+    check_search(zero, R.quantize(np.zeros((k, dim))), dim)
+
+
+def test_searches_of_different_sizes_follow_one_another():
+    """Scratch that grows and is reused: small after large, large after small, on one map."""
+    rng = np.random.default_rng(15)
+    dim, k = 130, 600
+    w = R.quantize(rng.standard_normal((k, dim)))
+    som = make(20, 30, dim)
+    wd = dev(w)
+    for n in (1, 900, 3, 5000, 64, 5000):
+        x = R.quantize(rng.standard_normal((n, dim)))
+        got = som.bmus(dev(x), nodes=wd).cpu().numpy()
+        assert np.array_equal(got, R.nearest(R.values(*x, dim), R.values(*w, dim)))
+    som.close()
+
+
+def test_search_quantises_the_code_book_where_no_nodes_are_given():
+    rng = np.random.default_rng(16)
+    dim, W = 70, rng.standard_normal((12 * 9, 70)).astype(np.float32)
+    x = R.quantize(rng.standard_normal((250, dim)))
+    som = make(12, 9, dim, W)
+    got = som.bmus(dev(x)).cpu().numpy()
+    assert np.array_equal(got, R.nearest(R.values(*x, dim), R.values(*R.quantize(W), dim)))
+    som.close()
+
+
+# ---------------------------------------------------------------- updates and epochs
+EPOCHS = [(1, 4, 5, 3, "planar", "square", 2.0), (1000, 20, 20, 10, "planar", "square", 3.0), (37, 9, 11, 77, "toroid", "hexagonal", 1.5),
+          (3000, 6, 7, 128, "planar", "hexagonal", 2.5), (2500, 40, 35, 100, "toroid", "square", 5.0), (600, 10, 10, 1000, "planar", "square", 1.0),
+          (500, 8, 8, 2100, "planar", "square", 2.0)]
+
+
+@pytest.mark.parametrize("n,rows,cols,dim,map_type,grid_type,radius", EPOCHS)
+def test_epoch(oracle, n, rows, cols, dim, map_type, grid_type, radius):
+    rng = np.random.default_rng(n + dim)
+    means = rng.random((12, dim))
+    x = R.quantize(means[rng.integers(0, 12, n)] + 0.1 * rng.standard_normal((n, dim)))
+    W = (means[rng.integers(0, 12, rows * cols)] + 0.1 * rng.standard_normal((rows * cols, dim))).astype(np.float32)
+    X = R.values(*x, dim).astype(np.float32)
+    som = make(rows, cols, dim, W, map_type=map_type, grid_type=grid_type)
+    b = som.train_epoch(dev(x), radius).cpu().numpy()
+    assert np.array_equal(b, R.nearest(X.astype(np.float64), R.values(*R.quantize(W), dim)))
+    S, C = oracle.accumulate_dense(X, b, som.k)
+    P.check_codebook(oracle, S, C, W, som.codebook.cpu().numpy(), rows, cols, P.MAP[map_type], P.GRID[grid_type], radius)
+    som.close()
+
+
+@pytest.mark.parametrize("function,compact", [("bubble", False), ("gaussian", True)])
+def test_update_under_other_neighbourhoods(oracle, function, compact):
+    rng = np.random.default_rng(21)
+    n, rows, cols, dim = 800, 9, 13, 45
+    x = R.quantize(rng.standard_normal((n, dim)))
+    X = R.values(*x, dim).astype(np.float32)
+    W = rng.standard_normal((rows * cols, dim)).astype(np.float32)
+    b = rng.integers(0, rows * cols // 3, n).astype(np.int32)
+    som = make(rows, cols, dim, W)
+    som.set_neighborhood(function, compact)
+    som.update(dev(x), P.to_dev(b), 2.0)
+    S, C = oracle.accumulate_dense(X, b, som.k)
+    P.check_codebook(oracle, S, C, W, som.codebook.cpu().numpy(), rows, cols, 0, 0, 2.0, function=int(function == "bubble"), compact=compact)
+    som.close()
+
+
+def test_update_of_one_crowded_node(oracle):
+    """All instances on one node: its chunks are added up in groups."""
+    rng = np.random.default_rng(22)
+    n, rows, cols, dim = 5000, 5, 5, 200
+    x = R.quantize(rng.standard_normal((n, dim)) + 1.0)
+    W = rng.standard_normal((rows * cols, dim)).astype(np.float32)
+    b = np.full(n, 7, np.int32)
+    som = make(rows, cols, dim, W)
+    som.update(dev(x), P.to_dev(b), 1.0)
+    S, C = oracle.accumulate_dense(R.values(*x, dim).astype(np.float32), b, som.k)
+    P.check_codebook(oracle, S, C, W, som.codebook.cpu().numpy(), rows, cols, 0, 0, 1.0)
+    som.close()
+
+
+def test_epoch_gives_the_same_bits_again():
+    rng = np.random.default_rng(23)
+    dim, W = 96, rng.standard_normal((15 * 17, 96)).astype(np.float32)
+    x = dev(R.quantize(rng.standard_normal((4000, dim))))
+    som = make(15, 17, dim, W)
+    seen = []
+    for _ in range(3):
+        som.codebook.copy_(P.to_dev(W))
+        b = som.train_epoch(x, 2.0)
+        seen.append((b.cpu().numpy(), som.codebook.cpu().numpy().copy()))
+    for b, c in seen[1:]:
+        assert np.array_equal(b, seen[0][0]) and np.array_equal(c, seen[0][1])
+    som.close()
+
+
+def test_schedule_is_its_epochs():
+    """train and train_snapshots on registered rows: the epochs with the schedule's radii, one after the other."""
+    rng = np.random.default_rng(24)
+    rows, cols, dim, n, epochs = 10, 12, 40, 700, 4
+    W = rng.standard_normal((rows * cols, dim)).astype(np.float32)
+    x = dev(R.quantize(rng.standard_normal((n, dim))))
+    som = make(rows, cols, dim, W)
+    radii = som.cool_schedule(epochs)[0].cpu().numpy()
+    codebooks = []
+    for r in radii:
+        b = som.train_epoch(x, float(r))
+        codebooks.append(som.codebook.cpu().numpy().copy())
+    som.codebook.copy_(P.to_dev(W))
+    got, um, cbs, ball = som.train_snapshots(x, epochs, snapshots=2)
+    assert np.allclose(cbs[0].cpu().numpy(), codebooks[0], rtol=1e-5, atol=1e-6)
+    assert torch.equal(ball[-1], got) and torch.equal(cbs[-1], som.codebook)
+    last = cbs[-1].clone()
+    som.codebook.copy_(P.to_dev(W))
+    again = som.train(x, epochs)
+    assert torch.equal(again, got) and torch.equal(som.codebook, last)
+    # the other kinds of data can be registered again afterwards, and the map searches them
+    X = torch.from_numpy(rng.standard_normal((50, dim)).astype(np.float32)).cuda()
+    som.train(X, 1)
+    som.close()
+
+
+# ---------------------------------------------------------------- use
+def test_recorded_and_replayed_beside_eager_calls():
+    """Store, search, epoch and products recorded into a graph; eager calls of other sizes, scratch that grows, between the replays."""
+    rng = np.random.default_rng(31)
+    rows, cols, dim, n = 16, 18, 120, 2000
+    W = rng.standard_normal((rows * cols, dim)).astype(np.float32)
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        from paper_1305_1422_amd import Mx4
+        som = make(rows, cols, dim, W)
+        Wd, X = P.to_dev(W), torch.from_numpy(rng.standard_normal((n, dim)).astype(np.float32)).cuda()
+        other = dev(R.quantize(rng.standard_normal((3 * n, dim))))
+        few = dev(R.quantize(rng.standard_normal((2, dim))))
+        mx = Mx4(torch.empty((n, 64), dtype=torch.uint8, device="cuda"), torch.empty((n, 4), dtype=torch.uint8, device="cuda"))
+        nodes = som.quantize_mx4(Wd)
+        b, b1 = (torch.empty(n, dtype=torch.int32, device="cuda") for _ in range(2))
+        out = torch.empty((n, rows * cols), dtype=torch.bfloat16, device="cuda")
+
+        def work():
+            som.quantize_mx4(X, mx)
+            som.bmus(mx, b, nodes)
+            som.products_mx4(mx, nodes, out=out)
+            som.codebook.copy_(Wd)
+            som.train_epoch(mx, 2.0, bmus=b1)
+
+        work()
+        want = [t.clone() for t in (b, b1, out, som.codebook)]
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            work()
+        for step in range(4):
+            for t in (b, b1, out, som.codebook):
+                t.zero_()
+            graph.replay()
+            assert all(torch.equal(g, w) for g, w in zip((b, b1, out, som.codebook), want))
+            som.bmus(other if step == 1 else few, nodes=nodes)
+            som.products_mx4(few, nodes)
+        stream.synchronize()
+        som.close()
+
+
+def test_recording_a_call_that_needs_scratch_is_refused():
+    from paper_1305_1422_amd import capi
+    rng = np.random.default_rng(32)
+    dim, W = 64, np.zeros((3000, 64), np.float32)
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        som = make(50, 60, dim, W)
+        x, w = dev(R.quantize(rng.standard_normal((500, dim)))), dev(R.quantize(rng.standard_normal((3000, dim))))
+        b = torch.empty(500, dtype=torch.int32, device="cuda")
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            with pytest.raises(capi.SomError) as err:
+                som.bmus(x, b, w)
+        assert err.value.code == capi.SOM_ERR_STATE
+        som.bmus(x, b, w)
+        assert np.array_equal(b.cpu().numpy(), R.nearest(R.values(*host(x), dim), R.values(*host(w), dim)))
+        som.close()
+
+
+def test_two_maps_on_two_streams():
+    rng = np.random.default_rng(33)
+    dim = 100
+    w = R.quantize(rng.standard_normal((800, dim)))
+    xs = [R.quantize(rng.standard_normal((3000, dim))) for _ in range(2)]
+    streams, soms, outs = [torch.cuda.Stream() for _ in range(2)], [], []
+    for s in streams:
+        with torch.cuda.stream(s):
+            soms.append(make(20, 40, dim))
+    xd, wd = [dev(x) for x in xs], dev(w)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        outs = [soms[i].bmus(xd[i], nodes=wd) for i in range(2)]
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert np.array_equal(outs[i].cpu().numpy(), R.nearest(R.values(*xs[i], dim), R.values(*w, dim)))
+        soms[i].close()
+
+
+def test_set_trained_stored_and_searched(oracle):
+    """As a program uses them together: rows are stored, a map is trained on them, its code book stored, new rows placed, responses read."""
+    rng = np.random.default_rng(34)
+    rows, cols, dim, n = 12, 15, 96, 3000
+    means = rng.standard_normal((10, dim))
+    X = (means[rng.integers(0, 10, n)] + 0.1 * rng.standard_normal((n, dim))).astype(np.float32)
+    som = make(rows, cols, dim, rng.standard_normal((rows * cols, dim)).astype(np.float32))
+    mx = som.quantize_mx4(P.to_dev(X))
+    som.train(mx, 5)
+    nodes = som.quantize_mx4(som.codebook)
+    b = som.bmus(mx, nodes=nodes)
+    resp = som.products_mx4(mx, nodes).double().cpu().numpy()
+    x, w = som.dequantize_mx4(mx).double().cpu().numpy(), som.dequantize_mx4(nodes).double().cpu().numpy()
+    assert np.abs(resp - x @ w.T).max() <= 2.0 ** -20 * (np.abs(x) @ np.abs(w).T).max() * 2
+    assert np.array_equal(b.cpu().numpy(), R.nearest(x, w))
+    assert torch.equal(som.bmus(mx), b)
+    dist, qe = som.bmu_distances(som.dequantize_mx4(mx), b)
+    assert float(qe) == pytest.approx(float(dist.double().mean()), rel=1e-6)
+    som.close()
+
+
+# ---------------------------------------------------------------- refusals
+def test_refusals():
+    from paper_1305_1422_amd import Mx4, capi
+    L = capi.load()
+    som = make(2, 3, 40)
+    x = torch.randn(10, 40, device="cuda")
+    mx = som.quantize_mx4(x)
+    b = torch.empty(10, dtype=torch.int32, device="cuda")
+    ctx, bad = som.ctx, capi.SOM_ERR_INVALID_ARG
+    c, s, px, pb = mx.codes.data_ptr(), mx.scales.data_ptr(), x.data_ptr(), b.data_ptr()
+    cb = som.codebook.data_ptr()
+    for n in (0, -1, 1 << 31):
+        assert L.som_mx4_quantize(ctx, px, 0, n, 40, c, s) == bad
+        assert L.som_mx4_dequantize(ctx, c, s, n, px, 0, 40) == bad
+        assert L.som_mx4_product(ctx, c, s, n, c, s, 10, px, 0, 40) == bad
+        assert L.som_mx4_product(ctx, c, s, 10, c, s, n, px, 0, 40) == bad
+        assert L.som_bmus_mx4(ctx, c, s, n, c, s, pb) == bad
+        assert L.som_update_mx4(ctx, c, s, n, pb, cb, 1.0, 1.0) == bad
+        assert L.som_train_epoch_mx4(ctx, c, s, n, cb, 1.0, 1.0, pb) == bad
+        assert L.som_set_data_mx4(ctx, c, s, n) == bad
+    assert L.som_mx4_quantize(ctx, px, 3, 10, 40, c, s) == bad and L.som_last_error(ctx)
+    assert L.som_mx4_quantize(ctx, px, 0, 10, 39, c, s) == bad
+    assert L.som_mx4_quantize(ctx, px, 0, 10, 1 << 40, c, s) == bad
+    assert L.som_mx4_quantize(ctx, px + 1, 0, 10, 40, c, s) == bad
+    assert L.som_mx4_quantize(ctx, px, 0, 10, 40, c + 8, s) == bad
+    assert L.som_mx4_quantize(ctx, None, 0, 10, 40, c, s) == bad
+    assert L.som_mx4_quantize(ctx, px, 0, 10, 40, None, s) == bad
+    assert L.som_mx4_dequantize(ctx, c, None, 10, px, 0, 40) == bad
+    assert L.som_mx4_product(ctx, c, s, 10, c, s, 10, px, 0, 9) == bad
+    assert L.som_mx4_product(ctx, c, s, 10, c, s, 10, None, 0, 10) == bad
+    assert L.som_bmus_mx4(ctx, c, s, 10, c, s, None) == bad
+    assert L.som_bmus_mx4(ctx, c, s, 10, c + 4, s, pb) == bad
+    for radius, scale in ((0.0, 1.0), (float("inf"), 1.0), (1.0, 0.0), (1.0, 1.5)):
+        assert L.som_train_epoch_mx4(ctx, c, s, 10, cb, radius, scale, pb) == bad
+        assert L.som_update_mx4(ctx, c, s, 10, pb, cb, radius, scale) == bad
+    assert L.som_train_epoch_mx4(ctx, c, s, 10, None, 1.0, 1.0, pb) == bad
+    with pytest.raises(ValueError):
+        som.quantize_mx4(torch.zeros(4, 41, device="cuda"))
+    with pytest.raises(TypeError):
+        som.quantize_mx4(torch.zeros(4, 40, dtype=torch.float64, device="cuda"))
+    with pytest.raises(TypeError):
+        som.quantize_mx4(torch.zeros(40, 4, device="cuda").t())
+    with pytest.raises(ValueError):
+        som.bmus(Mx4(mx.codes[:, :16].contiguous(), mx.scales[:, :1].contiguous()))
+    with pytest.raises(ValueError):
+        som.bmus(mx, nodes=mx)                      # ten nodes for a map of six
+    with pytest.raises(TypeError):
+        som.bmus(x, nodes=mx)
+    with pytest.raises(ValueError):
+        som.bmus(mx, bmus=b[:9])
+    with pytest.raises(ValueError):
+        som.products_mx4(mx, mx, out=torch.empty(10, 9, device="cuda"))
+    with pytest.raises(ValueError):
+        capi.som_mx4_dequantize(ctx, mx.codes, mx.scales, torch.empty(9, 40, device="cuda"))
+    som.close()
