@@ -1,9 +1,20 @@
 // Best-matching units of microscaled 4-bit rows among microscaled 4-bit nodes (mx4.hpp; som_bmus_mx4): the node of the
 // smallest |x - w|^2 = |x|^2 - 2 (x.w - |w|^2 / 2), the lowest of equally near ones.
 //
-// Direct search: every score x.w - |w|^2 / 2 in fp64.  The dot product of two blocks is exact in fp32 (mx4.hpp), the sum over the
+// Small searches are direct: every score x.w - |w|^2 / 2 in fp64.  The dot product of two blocks is exact in fp32 (mx4.hpp), the sum over the
 // blocks is taken in fp64, exact while the exponents of a row's products lie within 2^40 of each other.  Groups of lanes share a node's blocks.
-#include "mx4.hpp"
+//
+// Larger ones go through the matrix cores, whose fp32 sums are off by a bound that is known (margin below):
+//   k_mx4_nodes    -|w|^2 / 2 of every node (what the accumulators start from) and the nodes' scales, packed;
+//   k_mx4_search   tiles of scores (mx4_tiles.hpp), never stored: per instance and group of 16 consecutive nodes - what a lane holds of a
+//                  tile - their maximum, of those the largest with its group and the largest of the other groups;
+//   k_mx4_resolve  where no other group comes within the margin: the 16 scores of the group again, and if one of them alone is within the
+//                  margin of the largest, that is the node.  A wavefront has 16 instances; an instruction multiplies the 16 nodes of
+//                  one of them with all 16, a column of its result is of use, which is still a hundred times less than the vector units would need;
+//   k_mx4_search   again for the instances of which another group did: it lists the groups within the margin;
+//   k_mx4_exact    what is left, in fp64: the listed groups of these, the one group of the others; all nodes where there are more than kMx4List
+//                  groups, or where fp32 could overflow.
+#include "mx4_tiles.hpp"
 
 namespace som {
 
@@ -79,6 +90,7 @@ __global__ __launch_bounds__(256) void k_mx4_direct_join(const Mx4Best *__restri
   if (threadIdx.x == 0) bmus[blockIdx.x] = r.node == 0x7fffffff ? 0 : r.node;
 }
 
+// ---------------------------------------------------------------- direct search
 // Shares of the nodes per instance: enough workgroups to fill the chip, a pass over their lanes at least.
 static int direct_shares(const som_ctx *c, int64_t n, int lanes) {
   const int64_t all = ((int64_t)c->k * lanes + 255) / 256, want = (8 * (int64_t)c->n_cu + n - 1) / n;
@@ -91,19 +103,377 @@ static int direct_lanes_log(int blocks) {
   return l;
 }
 
+static hipError_t search_direct(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int32_t *bmus) {
+  const int blocks = mx4_blocks(c->dim), log_lanes = direct_lanes_log(blocks), shares = direct_shares(c, x.n, 1 << log_lanes);
+  Mx4Best *rec = static_cast<Mx4Best *>(scratch);
+  for (int64_t r0 = 0; r0 < x.n; r0 += 65535) {
+    const Mx4Rows part = {x.codes + r0 * blocks * 16, x.scales + r0 * blocks, x.n - r0 < 65535 ? x.n - r0 : 65535};
+    hipLaunchKernelGGL(k_mx4_direct, dim3(shares, (unsigned)part.n), dim3(256), 0, c->stream, part, w, blocks, log_lanes,
+                       rec + r0 * shares, bmus + r0);
+  }
+  if (shares > 1) hipLaunchKernelGGL(k_mx4_direct_join, dim3((unsigned)x.n), dim3(256), 0, c->stream, rec, shares, bmus);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- search on the matrix cores
+typedef Mx4Tile<8, 4, 2, 4, true> Mx4Sweep;      // 256 nodes x 256 instances
+
+constexpr int kMx4List = 16;            // groups an instance's list holds
+constexpr int kMx4NodeBlocks = 256;     // workgroups of the node pass at most
+constexpr float kMx4Lowest = -3.0e38f;  // below every score that counts
+
+struct Mx4Counts {
+  int listed, single;      // instances to list groups of (slots from the front), with one group (slots from the back)
+};
+
+// Largest and second largest of the groups' maxima.
+struct Mx4Record {
+  float best, second;
+  int group;
+};
+
+// A workgroup takes 64 nodes at a time.  parts[blockIdx.x]: the largest |w|^2 it saw (fp64, rounded up to fp32; infinity if it overflows).
+__global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int64_t padded, float *__restrict__ init, int *__restrict__ packed,
+                                                   float *__restrict__ parts, Mx4Counts *__restrict__ counts) {
+  __shared__ double s_norm[4][64];
+  __shared__ float s_max[64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4, steps = (blocks + 3) / 4;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *counts = Mx4Counts{0, 0};
+  float most = 0.f;
+  for (int64_t g = blockIdx.x; g < padded / 64; g += gridDim.x) {
+    double norm[4] = {0, 0, 0, 0};
+    for (int s = wave; s < steps; s += 4) {
+      const int block = 4 * s + q;
+      unsigned v = 0;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int64_t node = 64 * g + mx4_dealt(t, i);
+        if (block >= blocks || node >= w.n) continue;
+        const int e = w.scales[node * blocks + block];
+        const i32x4 x = *reinterpret_cast<const i32x4 *>(w.codes + (node * blocks + block) * 16);
+        float xx, ww;
+        mx4_block_dots(x, x, xx, ww);
+        norm[t] += e == 255 ? (double)NAN : (double)ww * mx4_pow2(2 * e - 254);
+        v |= (unsigned)e << (8 * t);
+      }
+      if (64 * g < w.n) packed[(g * steps + s) * 64 + lane] = (int)v;
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      norm[t] += __shfl_xor(norm[t], 16);
+      norm[t] += __shfl_xor(norm[t], 32);
+      if (q == t) s_norm[wave][mx4_dealt(t, i)] = norm[t];
+    }
+    __syncthreads();
+    if (threadIdx.x < 64) {
+      const double n2 = ((s_norm[0][threadIdx.x] + s_norm[1][threadIdx.x]) + s_norm[2][threadIdx.x]) + s_norm[3][threadIdx.x];
+      const int64_t node = 64 * g + threadIdx.x;
+      const bool usable = node < w.n && n2 == n2;      // a node with a NaN, and what is past the last one, can never win
+      init[node] = usable ? (float)(-0.5 * n2) : -INFINITY;
+      if (usable) most = fmaxf(most, __double2float_ru(n2));
+    }
+    __syncthreads();
+  }
+  if (threadIdx.x < 64) s_max[threadIdx.x] = most;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int t = 1; t < 64; ++t) most = fmaxf(most, s_max[t]);
+    parts[blockIdx.x] = most;
+  }
+}
+
+// kCollect: the instances are those of list (counts->listed of them); the groups whose maximum reaches an instance's threshold are appended to its
+// list.  Otherwise one record per instance, share of the nodes (blockIdx.y) and half of the wavefronts.
+template <bool kCollect>
+__global__ __launch_bounds__(512) void k_mx4_search(Mx4Operand x, Mx4Operand w, const float *__restrict__ init, int blocks,
+                                                    const void *__restrict__ zero16, int64_t tiles, Mx4Record *__restrict__ records,
+                                                    const Mx4Counts *__restrict__ counts, const int *__restrict__ list,
+                                                    const float *__restrict__ threshold, int *__restrict__ found,
+                                                    int *__restrict__ groups) {
+  typedef Mx4Sweep Tile;
+  __shared__ __attribute__((aligned(16))) char smem[Tile::kLds];
+  const int64_t n = kCollect ? counts->listed : x.rows.n;
+  const int64_t per = (tiles + gridDim.y - 1) / gridDim.y, first = blockIdx.y * per, last = first + per < tiles ? first + per : tiles;
+  if (first >= last) return;
+  const int64_t total = x.rows.n;
+  x.rows.n = n;
+  for (int64_t row0 = (int64_t)blockIdx.x * Tile::kRowsB; row0 < n; row0 += (int64_t)gridDim.x * Tile::kRowsB) {
+    Tile t;
+    t.setup(smem, w, x, init, blocks, zero16);
+    t.tile_b(row0, n, kCollect ? list : nullptr);
+    float best[Tile::kFragB], second[Tile::kFragB];
+    int at[Tile::kFragB];
+#pragma unroll
+    for (int v = 0; v < Tile::kFragB; ++v) {
+      best[v] = second[v] = kMx4Lowest;
+      at[v] = 0;
+      if (kCollect) {
+        const int64_t slot = row0 + 16 * (t.wb * Tile::kFragB + v) + t.l16;
+        best[v] = slot < n ? threshold[slot] : INFINITY;
+      }
+    }
+    t.run(first, last, [&](int64_t tile) {
+#pragma unroll
+      for (int g = 0; g < Tile::kFragA / 4; ++g)
+#pragma unroll
+        for (int v = 0; v < Tile::kFragB; ++v) {
+          float m = kMx4Lowest;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const mx_f32x4 a = t.acc[4 * g + u][v];
+            m = fmaxf(fmaxf(m, a[0]), a[1]);
+            m = fmaxf(fmaxf(m, a[2]), a[3]);
+          }
+          const int id = (int)tile * (Tile::kFragA / 4) + g;
+          if (kCollect) {
+            if (m >= best[v]) {
+              const int64_t slot = row0 + 16 * (t.wb * Tile::kFragB + v) + t.l16;
+              const int place = atomicAdd(&found[slot], 1);
+              if (place < kMx4List)
+                groups[slot * kMx4List + place] = ((int)tile * (Tile::kRowsA / 64) + t.wa * (Tile::kFragA / 4) + g) * 4 + t.q;
+            }
+          } else {
+            second[v] = fmaxf(second[v], fminf(best[v], m));
+            at[v] = m > best[v] ? id : at[v];
+            best[v] = fmaxf(best[v], m);
+          }
+        }
+    });
+    if (!kCollect) {
+#pragma unroll
+      for (int v = 0; v < Tile::kFragB; ++v) {
+        // group of 16 nodes: tile, this wavefront's 64-node part, the lane's quarter of it
+        int id = ((at[v] / (Tile::kFragA / 4)) * (Tile::kRowsA / 64) + t.wa * (Tile::kFragA / 4) + at[v] % (Tile::kFragA / 4)) * 4 + t.q;
+        float b = best[v], s = second[v];
+#pragma unroll
+        for (int o = 16; o < 64; o <<= 1) {
+          const float ob = __shfl_xor(b, o), os = __shfl_xor(s, o);
+          const int oid = __shfl_xor(id, o);
+          s = fmaxf(fmaxf(s, os), fminf(b, ob));
+          id = ob > b ? oid : id;
+          b = fmaxf(b, ob);
+        }
+        const int64_t row = row0 + 16 * (t.wb * Tile::kFragB + v) + t.l16;
+        if (t.q == 0 && row < n) records[((int64_t)blockIdx.y * Tile::kWavesA + t.wa) * total + row] = Mx4Record{b, s, id};
+      }
+    }
+  }
+}
+
+// What two scores of an instance may differ by in fp32 without being in order: twice the error of one.  steps + 1 roundings of sums of terms whose
+// magnitudes add up to |x| |w| + |w|^2 / 2 at most, |x| taken as what its largest scale allows; a term below the smallest normal fp32
+// number may be lost.  Infinite where the scores could overflow.
+__device__ __forceinline__ double mx4_margin(int exponent, float wmax2, int blocks) {
+  const double x = 6.0 * sqrt(32.0 * blocks) * mx4_pow2(exponent - 127), w = sqrt((double)wmax2);
+  const double size = x * w + 0.5 * (double)wmax2;
+  if (!(size < 1e37)) return INFINITY;
+  return 2.0 * (((blocks + 3) / 4 + 1) * kMx4Delta * size + 1e-34 * blocks);
+}
+
+// 16 instances a wavefront, lane l: instance l % 16.
+__global__ __launch_bounds__(256) void k_mx4_resolve(Mx4Rows x, Mx4Rows w, const float *__restrict__ init, int blocks,
+                                                     const Mx4Record *__restrict__ records, int shares, const float *__restrict__ parts,
+                                                     int nparts, Mx4Counts *__restrict__ counts, int *__restrict__ list,
+                                                     float *__restrict__ threshold, int *__restrict__ found, int *__restrict__ groups,
+                                                     int32_t *__restrict__ bmus) {
+  __shared__ float s_max[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q = lane >> 4;
+  float wmax2 = (int)threadIdx.x < nparts ? parts[threadIdx.x] : 0.f;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) wmax2 = fmaxf(wmax2, __shfl_xor(wmax2, o));
+  if (lane == 0) s_max[wave] = wmax2;
+  __syncthreads();
+  wmax2 = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
+  const int64_t row0 = ((int64_t)blockIdx.x * 4 + wave) * 16, row = row0 + l16;
+  if (row0 >= x.n) return;
+  const int64_t xr = row < x.n ? row : x.n - 1;
+  float best = kMx4Lowest, second = kMx4Lowest;
+  int group = 0;
+  for (int s = 0; s < shares; ++s) {
+    const Mx4Record r = records[s * x.n + xr];
+    second = fmaxf(fmaxf(second, r.second), fminf(best, r.best));
+    group = r.best > best ? r.group : group;
+    best = fmaxf(best, r.best);
+  }
+  mx_f32x4 mine = {0.f, 0.f, 0.f, 0.f};       // scores of nodes 16 group + 4 q ..
+  int exponent = 0;
+  mx_f32x4 acc[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) acc[r] = *reinterpret_cast<const mx_f32x4 *>(init + 16 * (int64_t)__builtin_amdgcn_readlane(group, r) + 4 * q);
+  const i32x4 none = {0, 0, 0, 0};
+  for (int b0 = 0; b0 < blocks; b0 += 4) {
+    const int b = b0 + q;
+    const bool in = b < blocks;
+    const i32x4 xc = in ? *reinterpret_cast<const i32x4 *>(x.codes + (xr * blocks + b) * 16) : none;
+    const int xs = in ? x.scales[xr * blocks + b] : 0;
+    exponent = max(exponent, xs);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      int64_t node = 16 * (int64_t)__builtin_amdgcn_readlane(group, r) + l16;
+      if (node >= w.n) node = w.n - 1;
+      const i32x4 wc = in ? *reinterpret_cast<const i32x4 *>(w.codes + (node * blocks + b) * 16) : none;
+      const int ws = in ? w.scales[node * blocks + b] : 0;
+      acc[r] = mx4_mfma<0, 0>(wc, xc, acc[r], ws, xs);
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+    if (l16 == r) mine = acc[r];
+  exponent = max(exponent, __shfl_xor(exponent, 16));
+  exponent = max(exponent, __shfl_xor(exponent, 32));
+  const double margin = mx4_margin(exponent, wmax2, blocks);
+  const float reach = __double2float_rd((double)best - margin);
+  int near = 0, first = 0x7fffffff;
+#pragma unroll
+  for (int u = 3; u >= 0; --u)
+    if (mine[u] >= reach) { ++near; first = 16 * group + 4 * q + u; }
+#pragma unroll
+  for (int o = 16; o < 64; o <<= 1) {
+    near += __shfl_xor(near, o);
+    first = min(first, __shfl_xor(first, o));
+  }
+  if (q != 0 || row >= x.n) return;
+  if (exponent == 255) {                       // no finite distance to any node
+    bmus[row] = 0;
+  } else if (!(margin < INFINITY) || !(best > kMx4Lowest)) {
+    const int64_t slot = x.n - 1 - atomicAdd(&counts->single, 1);
+    list[slot] = (int)row;
+    found[slot] = kMx4List + 1;
+  } else if (second >= reach) {
+    const int slot = atomicAdd(&counts->listed, 1);
+    list[slot] = (int)row;
+    threshold[slot] = reach;
+    found[slot] = 0;
+  } else if (near == 1) {
+    bmus[row] = first;
+  } else {
+    const int64_t slot = x.n - 1 - atomicAdd(&counts->single, 1);
+    list[slot] = (int)row;
+    found[slot] = 1;
+    groups[slot * kMx4List] = group;
+  }
+}
+
+// 16 lanes an instance, one node of a group each.
+__global__ __launch_bounds__(256) void k_mx4_exact(Mx4Rows x, Mx4Rows w, int blocks, const Mx4Counts *__restrict__ counts,
+                                                   const int *__restrict__ list, const int *__restrict__ found,
+                                                   const int *__restrict__ groups, int32_t *__restrict__ bmus) {
+  const int l16 = threadIdx.x & 15;
+  const int64_t listed = counts->listed, total = listed + counts->single;
+  for (int64_t u = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); u < total; u += (int64_t)gridDim.x * 16) {
+    const int64_t slot = u < listed ? u : x.n - 1 - (u - listed);
+    const int64_t row = list[slot];
+    const bool all = found[slot] > kMx4List;
+    const int64_t ng = all ? (w.n + 15) / 16 : found[slot];
+    double best = -INFINITY;
+    int arg = 0x7fffffff;
+    for (int64_t g = 0; g < ng; ++g) {
+      const int64_t node = 16 * (all ? g : (int64_t)groups[slot * kMx4List + g]) + l16;
+      if (node >= w.n) continue;
+      double s = 0.0;
+      for (int b = 0; b < blocks; ++b) {
+        const int ex = x.scales[row * blocks + b], ew = w.scales[node * blocks + b];
+        float xw, ww;
+        mx4_block_dots(*reinterpret_cast<const i32x4 *>(x.codes + (row * blocks + b) * 16),
+                       *reinterpret_cast<const i32x4 *>(w.codes + (node * blocks + b) * 16), xw, ww);
+        s += (double)xw * mx4_pow2(ex + ew - 254) - (double)ww * mx4_pow2(2 * ew - 255);
+        if (ex == 255 || ew == 255) s = NAN;
+      }
+      if (mx4_better(s, (int)node, best, arg)) { best = s; arg = (int)node; }
+    }
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) {
+      const double s = __shfl_xor(best, o);
+      const int i = __shfl_xor(arg, o);
+      if (mx4_better(s, i, best, arg)) { best = s; arg = i; }
+    }
+    if (l16 == 0) bmus[row] = arg == 0x7fffffff ? 0 : arg;
+  }
+}
+
+// Shares of the node tiles: the fewest rounds of workgroups (one a CU) times what each of them takes.
+static int sweep_shares(const som_ctx *c, int64_t n) {
+  const int64_t tiles = ((int64_t)c->k + Mx4Sweep::kRowsA - 1) / Mx4Sweep::kRowsA, nb = (n + Mx4Sweep::kRowsB - 1) / Mx4Sweep::kRowsB;
+  const int64_t steps = (mx4_blocks(c->dim) + 3) / 4;
+  int64_t best = 0;
+  int shares = 1;
+  for (int s = 1; s <= tiles && s <= 64; ++s) {
+    const int64_t rounds = (nb * s + c->n_cu - 1) / c->n_cu, cost = rounds * ((tiles + s - 1) / s * steps + 3);
+    if (s == 1 || cost < best) {
+      best = cost;
+      shares = s;
+    }
+  }
+  return shares;
+}
+
+// A direct search takes the vector units about 60 operations for 32 multiply-adds, and two launches; the other five.
+static bool direct_pays(const som_ctx *c, int64_t n) {
+  return n * (double)c->k * mx4_blocks(c->dim) <= 8e6;
+}
+
+struct Mx4SearchScratch {
+  float *init, *parts, *threshold;
+  int *packed_w, *packed_x, *list, *found, *groups;
+  Mx4Counts *counts;
+  Mx4Record *records;
+  size_t bytes;
+};
+
+static Mx4SearchScratch search_scratch(const som_ctx *c, int64_t n, void *base) {
+  const int blocks = mx4_blocks(c->dim);
+  const size_t N = (size_t)n;
+  const size_t padded = ((size_t)c->k + Mx4Sweep::kRowsA - 1) / Mx4Sweep::kRowsA * Mx4Sweep::kRowsA;
+  Mx4SearchScratch m;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    void *p = static_cast<char *>(base) + at;
+    at += (bytes + 255) / 256 * 256;
+    return p;
+  };
+  m.init = static_cast<float *>(take(padded * 4));
+  m.parts = static_cast<float *>(take(kMx4NodeBlocks * 4));
+  m.counts = static_cast<Mx4Counts *>(take(sizeof(Mx4Counts)));
+  m.packed_w = static_cast<int *>(take(mx4_packed_bytes(c->k, blocks)));
+  m.packed_x = static_cast<int *>(take(mx4_packed_bytes(n, blocks)));
+  m.records = static_cast<Mx4Record *>(take((size_t)sweep_shares(c, n) * Mx4Sweep::kWavesA * N * sizeof(Mx4Record)));
+  m.list = static_cast<int *>(take(N * 4));
+  m.threshold = static_cast<float *>(take(N * 4));
+  m.found = static_cast<int *>(take(N * 4));
+  m.groups = static_cast<int *>(take(N * kMx4List * 4));
+  m.bytes = at;
+  return m;
+}
+
 size_t mx4_search_bytes(const som_ctx *c, int64_t n) {
+  if (!direct_pays(c, n)) return search_scratch(c, n, nullptr).bytes;
   const int shares = direct_shares(c, n, 1 << direct_lanes_log(mx4_blocks(c->dim)));
   return shares > 1 ? (size_t)n * shares * sizeof(Mx4Best) : 0;
 }
 
 hipError_t launch_bmu_mx4(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int32_t *bmus) {
-  const int blocks = mx4_blocks(c->dim), log_lanes = direct_lanes_log(blocks), shares = direct_shares(c, x.n, 1 << log_lanes);
-  Mx4Best *rec = static_cast<Mx4Best *>(scratch);
-  for (int64_t r0 = 0; r0 < x.n; r0 += 65535) {
-    const Mx4Rows part = {x.codes + r0 * blocks * 16, x.scales + r0 * blocks, x.n - r0 < 65535 ? x.n - r0 : 65535};
-    hipLaunchKernelGGL(k_mx4_direct, dim3(shares, (unsigned)part.n), dim3(256), 0, c->stream, part, w, blocks, log_lanes, rec, bmus + r0);
-  }
-  if (shares > 1) hipLaunchKernelGGL(k_mx4_direct_join, dim3((unsigned)x.n), dim3(256), 0, c->stream, rec, shares, bmus);
+  if (direct_pays(c, x.n)) return search_direct(c, x, w, scratch, bmus);
+  const Mx4SearchScratch m = search_scratch(c, x.n, scratch);
+  const int blocks = mx4_blocks(c->dim);
+  const int64_t tiles = (w.n + Mx4Sweep::kRowsA - 1) / Mx4Sweep::kRowsA, padded = tiles * Mx4Sweep::kRowsA;
+  const int parts = padded / 64 < kMx4NodeBlocks ? (int)(padded / 64) : kMx4NodeBlocks, shares = sweep_shares(c, x.n);
+  hipLaunchKernelGGL(k_mx4_nodes, dim3(parts), dim3(256), 0, c->stream, w, blocks, padded, m.init, m.packed_w, m.parts, m.counts);
+  hipError_t e = launch_mx4_pack_scales(c->stream, x.scales, x.n, blocks, false, m.packed_x);
+  if (e != hipSuccess) return e;
+  const Mx4Operand ox = {x, m.packed_x}, ow = {w, m.packed_w};
+  hipLaunchKernelGGL(k_mx4_search<false>, dim3((unsigned)((x.n + Mx4Sweep::kRowsB - 1) / Mx4Sweep::kRowsB), shares), dim3(Mx4Sweep::kThreads), 0,
+                     c->stream, ox, ow, m.init, blocks, c->zero16, tiles, m.records, m.counts, m.list, m.threshold, m.found, m.groups);
+  hipLaunchKernelGGL(k_mx4_resolve, dim3((unsigned)((x.n + 63) / 64)), dim3(256), 0, c->stream, x, w, m.init, blocks, m.records,
+                     shares * Mx4Sweep::kWavesA, m.parts, parts, m.counts, m.list, m.threshold, m.found, m.groups, bmus);
+  e = launch_mx4_pack_scales(c->stream, x.scales, x.n, blocks, false, m.packed_x, m.list, &m.counts->listed);
+  if (e != hipSuccess) return e;
+  const int64_t most = (x.n + Mx4Sweep::kRowsB - 1) / Mx4Sweep::kRowsB;
+  const unsigned ways = (unsigned)(tiles < 16 ? tiles : 16), wide = (unsigned)(most < 2 * c->n_cu / ways ? most : 2 * c->n_cu / ways);
+  hipLaunchKernelGGL(k_mx4_search<true>, dim3(wide < 1 ? 1 : wide, ways), dim3(Mx4Sweep::kThreads), 0, c->stream, ox, ow, m.init, blocks,
+                     c->zero16, tiles, m.records, m.counts, m.list, m.threshold, m.found, m.groups);
+  const int64_t rows16 = (x.n + 15) / 16;
+  hipLaunchKernelGGL(k_mx4_exact, dim3((unsigned)(rows16 < 8 * c->n_cu ? rows16 : 8 * c->n_cu)), dim3(256), 0, c->stream, x, w, blocks, m.counts,
+                     m.list, m.found, m.groups, bmus);
   return hipGetLastError();
 }
 

@@ -1,63 +1,172 @@
-// Dot products of all pairs of two sets of microscaled 4-bit rows (mx4.hpp; som_mx4_product):
-// out[i][j] = sum_c a_ic b_jc, fp32 accumulation on the scaled matrix cores, rounded once to the type of the output.
-//
-// A wavefront takes 16 rows of a and 64 of b straight from global memory.  The rows of b are the instruction's first operand, so that a lane
-// ends up with four consecutive products of one row of the output.
-#include "mx4.hpp"
+// Dot products of all pairs of two sets of microscaled 4-bit rows (som_mx4_product): out[i][j] = sum_c a_ic b_jc, fp32
+// accumulation on the scaled matrix cores, rounded once to the type of the output.  The rows of b are operand A of the
+// instruction (mx4_tiles.hpp), so that a lane ends up with 16 consecutive products of a row of the output.
+#include "mx4_tiles.hpp"
 
 namespace som {
 
-template <typename T> __device__ __forceinline__ T mx4_out(float v) { return (T)v; }
+// ---------------------------------------------------------------- scales
+__global__ __launch_bounds__(256) void k_mx4_pack_scales(const uint8_t *__restrict__ scales, int64_t n, int blocks, int steps, int dealt,
+                                                         int *__restrict__ packed, const int *__restrict__ list,
+                                                         const int *__restrict__ count) {
+  if (count) n = *count;
+  const int64_t words = (n + 63) / 64 * steps * 64;
+  for (int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x; w < words; w += (int64_t)gridDim.x * 256) {
+    const int lane = (int)(w & 63), i = lane & 15;
+    const int64_t gs = w >> 6, g = gs / steps;
+    const int block = 4 * (int)(gs - g * steps) + (lane >> 4);
+    unsigned v = 0;
+    if (block < blocks)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int64_t r = 64 * g + (dealt ? mx4_dealt(t, i) : 16 * t + i);
+        if (r < n) v |= (unsigned)scales[(list ? list[r] : r) * blocks + block] << (8 * t);
+      }
+    packed[w] = (int)v;
+  }
+}
 
+hipError_t launch_mx4_pack_scales(hipStream_t stream, const uint8_t *scales, int64_t n, int blocks, bool dealt, int *packed,
+                                  const int *list, const int *count) {
+  const int steps = (blocks + 3) / 4;
+  int64_t grid = ((n + 63) / 64 * steps * 64 + 255) / 256;
+  if (grid > 4096) grid = 4096;
+  hipLaunchKernelGGL(k_mx4_pack_scales, dim3((unsigned)grid), dim3(256), 0, stream, scales, n, blocks, steps, dealt ? 1 : 0, packed, list,
+                     count);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- few rows: a wavefront's 16 rows of a and 64 of b straight from memory
 template <typename T>
-__global__ __launch_bounds__(256) void k_mx4_product(Mx4Rows a, Mx4Rows b, int blocks, T *__restrict__ out, int64_t stride) {
+__global__ __launch_bounds__(256) void k_mx4_product_few(Mx4Rows a, Mx4Rows b, int blocks, T *__restrict__ out, int64_t stride) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q = lane >> 4;
-  const int64_t i = ((int64_t)blockIdx.y * 4 + wave) * 16 + l16, j0 = (int64_t)blockIdx.x * 64;
-  if (i - l16 >= a.n) return;
+  const int64_t j0 = ((int64_t)blockIdx.x * 4 + wave) * 64, i = (int64_t)blockIdx.y * 16 + l16;
+  if (j0 >= b.n) return;
   const int64_t ia = i < a.n ? i : a.n - 1;
   int64_t jb[4];
 #pragma unroll
-  for (int t = 0; t < 4; ++t) jb[t] = j0 + 16 * t + l16 < b.n ? j0 + 16 * t + l16 : b.n - 1;
+  for (int t = 0; t < 4; ++t) {
+    jb[t] = j0 + mx4_dealt(t, l16);
+    if (jb[t] >= b.n) jb[t] = b.n - 1;
+  }
   mx_f32x4 acc[4] = {};
+  const i32x4 none = {0, 0, 0, 0};
   for (int k0 = 0; k0 < blocks; k0 += 4) {
     const int k = k0 + q;
     const bool in = k < blocks;
-    const i32x4 none = {0, 0, 0, 0};
     const i32x4 x = in ? *reinterpret_cast<const i32x4 *>(a.codes + (ia * blocks + k) * 16) : none;
     const int sx = in ? a.scales[ia * blocks + k] : 0;
+    i32x4 y[4];
+    int sy[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      const i32x4 y = in ? *reinterpret_cast<const i32x4 *>(b.codes + (jb[t] * blocks + k) * 16) : none;
-      const int sy = in ? b.scales[jb[t] * blocks + k] : 0;
-      acc[t] = mx4_mfma<0, 0>(y, x, acc[t], sy, sx);
+      y[t] = in ? *reinterpret_cast<const i32x4 *>(b.codes + (jb[t] * blocks + k) * 16) : none;
+      sy[t] = in ? b.scales[jb[t] * blocks + k] : 0;
     }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) acc[t] = mx4_mfma<0, 0>(y[t], x, acc[t], sy[t], sx);
   }
   if (i >= a.n) return;
 #pragma unroll
   for (int t = 0; t < 4; ++t)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int64_t j = j0 + 16 * t + 4 * q + r;
-      if (j < b.n) out[i * stride + j] = mx4_out<T>(acc[t][r]);
+      const int64_t j = j0 + 16 * q + 4 * t + r;
+      if (j < b.n) out[i * stride + j] = (T)acc[t][r];
     }
 }
 
-template <typename T>
-static hipError_t product(som_ctx *c, Mx4Rows a, Mx4Rows b, T *out, int64_t stride) {
+// ---------------------------------------------------------------- tiles
+// kVec: rows of the output begin at 16-byte boundaries.
+template <typename T, typename Tile, bool kVec>
+__global__ __launch_bounds__(512) void k_mx4_product(Mx4Operand a, Mx4Operand b, int blocks, const void *__restrict__ zero16,
+                                                     T *__restrict__ out, int64_t stride, unsigned tiles_j) {
+  __shared__ __attribute__((aligned(16))) char smem[Tile::kLds];
+  Tile t;
+  const unsigned ti = blockIdx.x / tiles_j, tj = blockIdx.x - ti * tiles_j;
+  t.setup(smem, b, a, nullptr, blocks, zero16);
+  const int64_t i0 = (int64_t)ti * Tile::kRowsB, j0 = (int64_t)tj * Tile::kRowsA;
+  t.tile_b(i0, a.rows.n, nullptr);
+  t.run(tj, tj + 1, [](int64_t) {});
+  const int64_t m = b.rows.n;
+#pragma unroll
+  for (int v = 0; v < Tile::kFragB; ++v) {
+    const int64_t i = i0 + 16 * (t.wb * Tile::kFragB + v) + t.l16;
+#pragma unroll
+    for (int g = 0; g < Tile::kFragA / 4; ++g) {
+      const int64_t j = j0 + 64 * (t.wa * (Tile::kFragA / 4) + g) + 16 * t.q;
+      T row[16];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) row[u] = (T)t.acc[4 * g + u / 4][v][u & 3];
+      if (i < a.rows.n) {
+        T *dst = out + i * stride + j;
+        if (kVec && j + 16 <= m) {
+#pragma unroll
+          for (int u = 0; u < (int)sizeof(T); ++u) reinterpret_cast<i32x4 *>(dst)[u] = reinterpret_cast<const i32x4 *>(row)[u];
+        } else {
+#pragma unroll
+          for (int u = 0; u < 16; ++u)
+            if (j + u < m) dst[u] = row[u];
+        }
+      }
+    }
+  }
+}
+
+typedef Mx4Tile<8, 4, 2, 4, false> Mx4Wide;       // 256 x 256
+typedef Mx4Tile<4, 2, 2, 4, false> Mx4Narrow;     // 128 x 128
+
+// Up to this many rows of a the operands come straight from memory.
+constexpr int64_t kFewRows = 64;
+
+static int64_t tiles(int64_t rows, int per) { return (rows + per - 1) / per; }
+
+size_t mx4_product_bytes(const som_ctx *c, int64_t n, int64_t m) {
   const int blocks = mx4_blocks(c->dim);
-  const int64_t step = 65535ll * 64;             // rows of a a launch can take in its second grid direction
-  for (int64_t i0 = 0; i0 < a.n; i0 += step) {
-    const Mx4Rows part = {a.codes + i0 * blocks * 16, a.scales + i0 * blocks, a.n - i0 < step ? a.n - i0 : step};
-    const dim3 grid((unsigned)((b.n + 63) / 64), (unsigned)((part.n + 63) / 64));
-    hipLaunchKernelGGL(k_mx4_product<T>, grid, dim3(256), 0, c->stream, part, b, blocks, out + i0 * stride, stride);
+  return n <= kFewRows ? 0 : mx4_packed_bytes(n, blocks) + mx4_packed_bytes(m, blocks);
+}
+
+template <typename T, typename Tile>
+static hipError_t product_tiles(som_ctx *c, Mx4Operand a, Mx4Operand b, T *out, int64_t stride) {
+  const int blocks = mx4_blocks(c->dim);
+  const int64_t tj = tiles(b.rows.n, Tile::kRowsA), ti = tiles(a.rows.n, Tile::kRowsB);
+  const bool vec = (uintptr_t)out % 16 == 0 && (stride * (int64_t)sizeof(T)) % 16 == 0;
+  const int64_t most = (1ll << 30) / tj > 0 ? (1ll << 30) / tj : 1;           // tile rows of a launch
+  for (int64_t t0 = 0; t0 < ti; t0 += most) {
+    const int64_t now = ti - t0 < most ? ti - t0 : most, i0 = t0 * Tile::kRowsB;
+    Mx4Operand part = a;
+    part.rows.codes += i0 * blocks * 16;
+    part.rows.scales += i0 * blocks;
+    part.rows.n = a.rows.n - i0;
+    part.packed += (size_t)(i0 / 64) * ((blocks + 3) / 4) * 64;
+    const dim3 grid((unsigned)(now * tj));
+    if (vec) hipLaunchKernelGGL((k_mx4_product<T, Tile, true>), grid, dim3(Tile::kThreads), 0, c->stream, part, b, blocks, c->zero16, out + i0 * stride, stride, (unsigned)tj);
+    else hipLaunchKernelGGL((k_mx4_product<T, Tile, false>), grid, dim3(Tile::kThreads), 0, c->stream, part, b, blocks, c->zero16, out + i0 * stride, stride, (unsigned)tj);
   }
   return hipGetLastError();
 }
 
-hipError_t launch_mx4_product(som_ctx *c, Mx4Rows a, Mx4Rows b, void *out, int type, int64_t stride) {
-  if (type == SOM_FP32) return product(c, a, b, static_cast<float *>(out), stride);
-  if (type == SOM_FP16) return product(c, a, b, static_cast<_Float16 *>(out), stride);
-  return product(c, a, b, static_cast<__bf16 *>(out), stride);
+template <typename T>
+static hipError_t product(som_ctx *c, Mx4Rows a, Mx4Rows b, T *out, int64_t stride, void *scratch) {
+  const int blocks = mx4_blocks(c->dim);
+  if (a.n <= kFewRows) {
+    const dim3 grid((unsigned)((b.n + 255) / 256), (unsigned)((a.n + 15) / 16));
+    hipLaunchKernelGGL(k_mx4_product_few<T>, grid, dim3(256), 0, c->stream, a, b, blocks, out, stride);
+    return hipGetLastError();
+  }
+  int *pa = static_cast<int *>(scratch), *pb = pa + mx4_packed_bytes(a.n, blocks) / 4;
+  hipError_t e = launch_mx4_pack_scales(c->stream, a.scales, a.n, blocks, false, pa);
+  if (e == hipSuccess) e = launch_mx4_pack_scales(c->stream, b.scales, b.n, blocks, true, pb);
+  if (e != hipSuccess) return e;
+  const Mx4Operand oa = {a, pa}, ob = {b, pb};
+  if (tiles(a.n, Mx4Wide::kRowsB) * tiles(b.n, Mx4Wide::kRowsA) >= c->n_cu) return product_tiles<T, Mx4Wide>(c, oa, ob, out, stride);
+  return product_tiles<T, Mx4Narrow>(c, oa, ob, out, stride);
+}
+
+hipError_t launch_mx4_product(som_ctx *c, Mx4Rows a, Mx4Rows b, void *out, int type, int64_t stride, void *scratch) {
+  if (type == SOM_FP32) return product(c, a, b, static_cast<float *>(out), stride, scratch);
+  if (type == SOM_FP16) return product(c, a, b, static_cast<_Float16 *>(out), stride, scratch);
+  return product(c, a, b, static_cast<__bf16 *>(out), stride, scratch);
 }
 
 }  // namespace som

@@ -1186,7 +1186,10 @@ int som_mx4_product(som_ctx *c, const uint8_t *codes_a, const uint8_t *scales_a,
   if (!rc) rc = check_mx4(c, codes_b, scales_b, m);
   if (!rc) rc = check_typed(c, out, type, n, m, stride);
   if (rc) return rc;
-  SOM_LAUNCH(c, launch_mx4_product(c, Mx4Rows{codes_a, scales_a, n}, Mx4Rows{codes_b, scales_b, m}, out, type, stride));
+  void *scratch = nullptr;
+  rc = mx4_scratch(c, kMx4Search, mx4_product_bytes(c, n, m), &scratch);
+  if (rc) return rc;
+  SOM_LAUNCH(c, launch_mx4_product(c, Mx4Rows{codes_a, scales_a, n}, Mx4Rows{codes_b, scales_b, m}, out, type, stride, scratch));
   return SOM_OK;
 }
 

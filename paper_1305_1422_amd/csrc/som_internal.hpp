@@ -487,7 +487,8 @@ hipError_t launch_mx4_quantize(hipStream_t stream, const void *rows, int type, i
                                uint8_t *scales);
 hipError_t launch_mx4_dequantize(hipStream_t stream, Mx4Rows x, int dim, void *rows, int type, int64_t stride);
 // mx4_product.hip
-hipError_t launch_mx4_product(som_ctx *c, Mx4Rows a, Mx4Rows b, void *out, int type, int64_t stride);
+size_t mx4_product_bytes(const som_ctx *c, int64_t n, int64_t m);      // its scratch
+hipError_t launch_mx4_product(som_ctx *c, Mx4Rows a, Mx4Rows b, void *out, int type, int64_t stride, void *scratch);
 // bmu_mx4.hip
 size_t mx4_search_bytes(const som_ctx *c, int64_t n);       // scratch of a search of n rows among the c->k nodes
 hipError_t launch_bmu_mx4(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int32_t *bmus);

@@ -107,7 +107,7 @@ def test_round_trip_of_few_and_many_rows(n):
 # ---------------------------------------------------------------- products
 @pytest.mark.parametrize("kind", list(TYPES))
 @pytest.mark.parametrize("n,m,dim", [(1, 1, 1), (1, 70, 33), (3, 17, 128), (65, 63, 129), (64, 64, 32), (130, 300, 100), (257, 259, 512),
-                                     (300, 70, 1000), (40, 513, 1500), (16, 16, 4096)])
+                                     (300, 70, 1000), (40, 513, 1500), (16, 16, 4096), (200, 200, 1), (4200, 4100, 96), (2000, 10000, 130)])
 def test_product(kind, n, m, dim):
     """The instruction's four block sums and its addend are cut off at 2^-20 of their magnitudes at most, once for every 128
     features, then there is one rounding to the type."""
@@ -185,7 +185,8 @@ def check_search(x, w, dim, rows=1):
 
 
 SIZES = [(1, 1, 1), (1, 3, 40), (5, 64, 32), (17, 65, 33), (64, 16, 128), (100, 400, 10), (65, 130, 129), (300, 77, 1000), (1000, 1025, 100),
-         (1, 2500, 1000), (3, 5000, 96), (2000, 63, 257), (4099, 640, 128), (513, 2000, 1024), (700, 900, 1100), (130, 300, 4096)]
+         (1, 2500, 1000), (3, 5000, 96), (2000, 63, 257), (4099, 640, 128), (513, 2000, 1024), (700, 900, 1100), (130, 300, 4096),
+         (5000, 3000, 33), (255, 3001, 1000), (2049, 1500, 300), (257, 1025, 4096), (9000, 70, 500), (70, 9000, 500), (3000, 5000, 20)]
 
 
 @pytest.mark.parametrize("n,k,dim", SIZES)
@@ -194,7 +195,7 @@ def test_search(n, k, dim):
     check_search(R.quantize(rng.standard_normal((n, dim))), R.quantize(rng.standard_normal((k, dim))), dim)
 
 
-@pytest.mark.parametrize("n,k,dim", [(3, 70, 32), (1500, 700, 96), (600, 400, 1030)])
+@pytest.mark.parametrize("n,k,dim", [(3, 70, 32), (1500, 700, 96), (600, 400, 1030), (4000, 2500, 96), (1500, 700, 1030)])
 def test_search_among_copies(n, k, dim):
     """Ties: few distinct nodes, each many times; the lowest index of the nearest ones."""
     rng = np.random.default_rng(n)
@@ -203,7 +204,7 @@ def test_search_among_copies(n, k, dim):
     check_search(R.quantize(rng.standard_normal((n, dim))), w, dim)
 
 
-@pytest.mark.parametrize("n,k,dim", [(2, 100, 64), (2000, 1000, 64), (300, 300, 1200)])
+@pytest.mark.parametrize("n,k,dim", [(2, 100, 64), (2000, 1000, 64), (300, 300, 1200), (5000, 3000, 64), (1000, 500, 1200)])
 def test_search_on_a_coarse_grid(n, k, dim):
     """Small whole numbers: many nodes are equally near."""
     rng = np.random.default_rng(k)
@@ -214,7 +215,7 @@ def test_search_on_a_coarse_grid(n, k, dim):
     check_search(R.quantize(x), R.quantize(w), dim)
 
 
-@pytest.mark.parametrize("n", [2, 1200])
+@pytest.mark.parametrize("n", [2, 1200, 6000])
 def test_search_among_near_copies(n):
     """Nodes that differ in one small block: their scores differ by less than fp32 keeps of their sums."""
     rng = np.random.default_rng(11)
@@ -227,7 +228,7 @@ def test_search_among_near_copies(n):
     check_search(R.quantize(x), R.quantize(w), dim)
 
 
-@pytest.mark.parametrize("n", [4, 900])
+@pytest.mark.parametrize("n", [4, 900, 9000])
 @pytest.mark.parametrize("low,high", [(107, 147), (1, 20), (230, 250), (60, 75)])
 def test_search_over_wide_scales(n, low, high):
     """Scales far from one another, sums that underflow or overflow fp32; within a node's and instance's 2^40 (fp64 exact)."""
@@ -241,7 +242,7 @@ def test_search_over_wide_scales(n, low, high):
     check_search(x, w, dim)
 
 
-@pytest.mark.parametrize("n,k", [(4, 40), (700, 400)])
+@pytest.mark.parametrize("n,k", [(4, 40), (700, 400), (3000, 1500)])
 def test_search_with_not_a_number(n, k):
     rng = np.random.default_rng(13)
     dim = 100
@@ -254,7 +255,7 @@ def test_search_with_not_a_number(n, k):
     check_search(x, w, dim)
 
 
-@pytest.mark.parametrize("n", [1, 500])
+@pytest.mark.parametrize("n", [1, 500, 30000])
 def test_search_of_zeros(n):
     dim, k = 64, 200
     rng = np.random.default_rng(14)
@@ -270,7 +271,7 @@ def test_searches_of_different_sizes_follow_one_another():
     w = R.quantize(rng.standard_normal((k, dim)))
     som = make(20, 30, dim)
     wd = dev(w)
-    for n in (1, 900, 3, 5000, 64, 5000):
+    for n in (1, 900, 3, 5000, 64, 20000, 5000):
         x = R.quantize(rng.standard_normal((n, dim)))
         got = som.bmus(dev(x), nodes=wd).cpu().numpy()
         assert np.array_equal(got, R.nearest(R.values(*x, dim), R.values(*w, dim)))
@@ -290,7 +291,8 @@ def test_search_quantises_the_code_book_where_no_nodes_are_given():
 # ---------------------------------------------------------------- updates and epochs
 EPOCHS = [(1, 4, 5, 3, "planar", "square", 2.0), (1000, 20, 20, 10, "planar", "square", 3.0), (37, 9, 11, 77, "toroid", "hexagonal", 1.5),
           (3000, 6, 7, 128, "planar", "hexagonal", 2.5), (2500, 40, 35, 100, "toroid", "square", 5.0), (600, 10, 10, 1000, "planar", "square", 1.0),
-          (500, 8, 8, 2100, "planar", "square", 2.0)]
+          (500, 8, 8, 2100, "planar", "square", 2.0),
+          (20000, 30, 40, 64, "toroid", "hexagonal", 3.0)]
 
 
 @pytest.mark.parametrize("n,rows,cols,dim,map_type,grid_type,radius", EPOCHS)
