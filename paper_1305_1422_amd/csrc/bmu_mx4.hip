@@ -132,31 +132,45 @@ struct Mx4Record {
   int group;
 };
 
+// Nodes as k_mx4_sweep reads them: 64 at a time, their fragments ([step][4] of 1 KB), per step a word of scales per lane, and what the
+// accumulators start from in the order of the nodes, rounded up to whole KB.
+__host__ __device__ constexpr int mx4_stream_bytes(int steps) { return steps * 4096 + ((steps + 1) * 256 + 1023) / 1024 * 1024; }
+
 // A workgroup takes 64 nodes at a time.  parts[blockIdx.x]: the largest |w|^2 it saw (fp64, rounded up to fp32; infinity if it overflows).
-__global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int64_t padded, float *__restrict__ init, int *__restrict__ packed,
-                                                   float *__restrict__ parts, Mx4Counts *__restrict__ counts) {
+// kStream: the nodes as k_mx4_sweep reads them, else their packed scales.
+template <bool kStream>
+__global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int64_t padded, float *__restrict__ init, char *__restrict__ stream,
+                                                   int *__restrict__ packed, float *__restrict__ parts, Mx4Counts *__restrict__ counts) {
   __shared__ double s_norm[4][64];
   __shared__ float s_max[64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4, steps = (blocks + 3) / 4;
   if (blockIdx.x == 0 && threadIdx.x == 0) *counts = Mx4Counts{0, 0};
   float most = 0.f;
   for (int64_t g = blockIdx.x; g < padded / 64; g += gridDim.x) {
+    char *mine = kStream ? stream + g * mx4_stream_bytes(steps) : nullptr;
     double norm[4] = {0, 0, 0, 0};
     for (int s = wave; s < steps; s += 4) {
       const int block = 4 * s + q;
       unsigned v = 0;
+      i32x4 x[4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         const int64_t node = 64 * g + mx4_dealt(t, i);
-        if (block >= blocks || node >= w.n) continue;
-        const int e = w.scales[node * blocks + block];
-        const i32x4 x = *reinterpret_cast<const i32x4 *>(w.codes + (node * blocks + block) * 16);
-        float xx, ww;
-        mx4_block_dots(x, x, xx, ww);
-        norm[t] += e == 255 ? (double)NAN : (double)ww * mx4_pow2(2 * e - 254);
-        v |= (unsigned)e << (8 * t);
+        const bool in = block < blocks && node < w.n;
+        const i32x4 none = {0, 0, 0, 0};
+        x[t] = in ? *reinterpret_cast<const i32x4 *>(w.codes + (node * blocks + block) * 16) : none;
+        v |= (in ? (unsigned)w.scales[node * blocks + block] : 0u) << (8 * t);
       }
-      if (64 * g < w.n) packed[(g * steps + s) * 64 + lane] = (int)v;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int e = (v >> (8 * t)) & 255;
+        float xx, ww;
+        mx4_block_dots(x[t], x[t], xx, ww);
+        norm[t] += e == 255 ? (double)NAN : (double)ww * mx4_pow2(2 * e - 254);
+        if (kStream) *reinterpret_cast<i32x4 *>(mine + (s * 4 + t) * 1024 + lane * 16) = x[t];
+      }
+      if (kStream) *reinterpret_cast<unsigned *>(mine + steps * 4096 + s * 256 + lane * 4) = v;
+      else if (64 * g < w.n) packed[(g * steps + s) * 64 + lane] = (int)v;
     }
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -169,7 +183,9 @@ __global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int64_
       const double n2 = ((s_norm[0][threadIdx.x] + s_norm[1][threadIdx.x]) + s_norm[2][threadIdx.x]) + s_norm[3][threadIdx.x];
       const int64_t node = 64 * g + threadIdx.x;
       const bool usable = node < w.n && n2 == n2;      // a node with a NaN, and what is past the last one, can never win
-      init[node] = usable ? (float)(-0.5 * n2) : -INFINITY;
+      const float from = usable ? (float)(-0.5 * n2) : -INFINITY;
+      init[node] = from;
+      if (kStream) *reinterpret_cast<float *>(mine + steps * 4096 + steps * 256 + threadIdx.x * 4) = from;
       if (usable) most = fmaxf(most, __double2float_ru(n2));
     }
     __syncthreads();
@@ -182,6 +198,173 @@ __global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int64_
   }
 }
 
+// ---------------------------------------------------------------- rows of up to 8 steps (1,024 features)
+// The instances stay in registers, the nodes stream through LDS.  A wavefront has 16 kF instances; per 64 nodes (one unit of the stream) it reads 4 kT
+// fragments for 4 kT kF instructions.  Results of four instructions are a lane's 16 scores of one instance: eight v_max3, and four operations
+// for the running maximum, its place and the runner-up, 12 to 4 kT instructions of 16 cycles, which one wavefront would issue in the same
+// time if kT = 1; so with few steps the instances are taken one fragment after the other, the maxima of one between the products of the next.
+// Two stages in LDS of kUnits units each: the loads of a stage are issued when the one before it begins.
+template <int kT, int kF, int kUnits, bool kByF>
+struct Mx4SweepShape {
+  static constexpr int T = kT, F = kF, units = kUnits, rows = 64 * kF;
+  static constexpr bool by_f = kByF;
+  static constexpr int unit = mx4_stream_bytes(kT), stage = kUnits * unit, chunks = stage / 1024, lds = 2 * stage;
+};
+template <int kT> struct Mx4ShapeOf;
+template <> struct Mx4ShapeOf<1> { typedef Mx4SweepShape<1, 8, 4, true> type; };
+template <> struct Mx4ShapeOf<2> { typedef Mx4SweepShape<2, 8, 2, true> type; };
+template <> struct Mx4ShapeOf<3> { typedef Mx4SweepShape<3, 4, 2, true> type; };
+template <> struct Mx4ShapeOf<4> { typedef Mx4SweepShape<4, 4, 1, false> type; };
+template <> struct Mx4ShapeOf<5> { typedef Mx4SweepShape<5, 4, 1, false> type; };
+template <> struct Mx4ShapeOf<6> { typedef Mx4SweepShape<6, 4, 1, false> type; };
+template <> struct Mx4ShapeOf<7> { typedef Mx4SweepShape<7, 3, 1, false> type; };
+template <> struct Mx4ShapeOf<8> { typedef Mx4SweepShape<8, 3, 1, false> type; };
+constexpr int kMx4SweepSteps = 8;
+
+// kCollect as in k_mx4_search.
+template <int kT, bool kCollect>
+__global__ __launch_bounds__(256, 2) void k_mx4_sweep(Mx4Rows x, int blocks, const char *__restrict__ stream, int64_t all_units,
+                                                      Mx4Record *__restrict__ records, const Mx4Counts *__restrict__ counts,
+                                                      const int *__restrict__ list, const float *__restrict__ threshold,
+                                                      int *__restrict__ found, int *__restrict__ groups) {
+  typedef typename Mx4ShapeOf<kT>::type Shape;
+  constexpr int kF = Shape::F, kUnits = Shape::units;
+  __shared__ __attribute__((aligned(16))) char smem[Shape::lds];
+  const unsigned lds = (unsigned)(size_t)(mx4_lds_t)smem;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, q = lane >> 4;
+  const int64_t n = kCollect ? counts->listed : x.n;
+  // stages of the stream: this share's
+  const int64_t all = (all_units + kUnits - 1) / kUnits, per = (all + gridDim.y - 1) / gridDim.y, first = blockIdx.y * per;
+  const int64_t last = first + per < all ? first + per : all;
+  if (first >= last) return;
+  auto load = [&](int64_t at, int half) {
+    const char *src = stream + at * Shape::stage + lane * 16;
+#pragma unroll
+    for (int u = 0; u < (Shape::chunks + 3) / 4; ++u) {
+      const int c = 4 * u + wave;
+      if (c < Shape::chunks) mx4_load_to_lds(src + c * 1024, lds + half * Shape::stage + c * 1024);
+    }
+  };
+  for (int64_t row0 = (int64_t)blockIdx.x * Shape::rows; row0 < n; row0 += (int64_t)gridDim.x * Shape::rows) {
+    load(first, 0);
+    i32x4 y[kF][kT];
+    int sy[(kF + 3) / 4][kT];
+    float best[kF], second[kF];
+    int at[kF];
+#pragma unroll
+    for (int f = 0; f < kF; ++f) {
+      const int64_t slot = row0 + 16 * (wave * kF + f) + l16;
+      int64_t row = slot < n ? slot : n - 1;
+      if (kCollect) row = list[row];
+#pragma unroll
+      for (int s = 0; s < kT; ++s) {
+        const bool in = 4 * s + q < blocks;
+        const i32x4 none = {0, 0, 0, 0};
+        y[f][s] = in ? *reinterpret_cast<const i32x4 *>(x.codes + (row * blocks + 4 * s + q) * 16) : none;
+        const int e = in ? x.scales[row * blocks + 4 * s + q] : 0;
+        sy[f / 4][s] = f % 4 == 0 ? e : sy[f / 4][s] | e << (8 * (f % 4));
+      }
+      best[f] = kCollect ? (slot < n ? threshold[slot] : INFINITY) : kMx4Lowest;
+      second[f] = kMx4Lowest;
+      at[f] = 0;
+    }
+    // scores a of instance fragment f and nodes 64 unit + 16 q .. + 15
+    auto maxima = [&](const mx_f32x4 (&a)[4], int f, int unit) {
+      float m = kMx4Lowest;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        m = fmaxf(fmaxf(m, a[t][0]), a[t][1]);
+        m = fmaxf(fmaxf(m, a[t][2]), a[t][3]);
+      }
+      if (kCollect) {
+        if (m >= best[f]) {
+          const int64_t slot = row0 + 16 * (wave * kF + f) + l16;
+          const int place = atomicAdd(&found[slot], 1);
+          if (place < kMx4List) groups[slot * kMx4List + place] = 4 * unit + q;
+        }
+      } else {
+        second[f] = __builtin_amdgcn_fmed3f(second[f], best[f], m);
+        at[f] = m > best[f] ? unit : at[f];
+        best[f] = fmaxf(best[f], m);
+      }
+    };
+    mx_f32x4 held[2][4];                       // kByF: scores whose maxima are still to be taken, of fragment kF - 1
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) held[1][t][r] = kMx4Lowest;
+    static_assert(!Shape::by_f || kF % 2 == 0, "the last fragment's scores are held[1]");
+    for (int64_t it = first; it < last; ++it) {
+      const int half = (int)(it - first) & 1;
+      mx4_wait<0>();
+      mx4_barrier();
+      if (it + 1 < last) load(it + 1, half ^ 1);
+#pragma unroll 1
+      for (int u = 0; u < kUnits; ++u) {
+        const int unit = (int)it * kUnits + u;
+        const char *base = smem + half * Shape::stage + u * Shape::unit;
+        mx_f32x4 from[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) from[t] = *reinterpret_cast<const mx_f32x4 *>(base + kT * 4352 + (16 * q + 4 * t) * 4);
+        if (Shape::by_f) {
+          i32x4 w[kT][4];
+          int sw[kT];
+#pragma unroll
+          for (int s = 0; s < kT; ++s) {
+            sw[s] = *reinterpret_cast<const int *>(base + kT * 4096 + s * 256 + lane * 4);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) w[s][t] = *reinterpret_cast<const i32x4 *>(base + (s * 4 + t) * 1024 + lane * 16);
+          }
+#pragma unroll
+          for (int f = 0; f < kF; ++f) {
+#pragma unroll
+            for (int s = 0; s < kT; ++s)
+#pragma unroll
+              for (int t = 0; t < 4; ++t)
+                held[f & 1][t] = mx4_mfma_at(t, f & 3, w[s][t], y[f][s], s == 0 ? from[t] : held[f & 1][t], sw[s], sy[f / 4][s]);
+            maxima(held[(f & 1) ^ 1], f == 0 ? kF - 1 : f - 1, f == 0 ? unit - 1 : unit);
+          }
+        } else {
+          mx_f32x4 acc[kF][4];
+#pragma unroll
+          for (int s = 0; s < kT; ++s) {
+            const int sw = *reinterpret_cast<const int *>(base + kT * 4096 + s * 256 + lane * 4);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+              const i32x4 w = *reinterpret_cast<const i32x4 *>(base + (s * 4 + t) * 1024 + lane * 16);
+#pragma unroll
+              for (int f = 0; f < kF; ++f) acc[f][t] = mx4_mfma_at(t, f & 3, w, y[f][s], s == 0 ? from[t] : acc[f][t], sw, sy[f / 4][s]);
+            }
+          }
+#pragma unroll
+          for (int f = 0; f < kF; ++f) maxima(acc[f], f, unit);
+        }
+      }
+    }
+    if (Shape::by_f) maxima(held[1], kF - 1, (int)last * kUnits - 1);
+    mx4_wait<0>();
+    mx4_barrier();                             // the stages may be filled again
+    if (!kCollect) {
+#pragma unroll
+      for (int f = 0; f < kF; ++f) {
+        int id = 4 * at[f] + q;
+        float b = best[f], s = second[f];
+#pragma unroll
+        for (int o = 16; o < 64; o <<= 1) {
+          const float ob = __shfl_xor(b, o), os = __shfl_xor(s, o);
+          const int oid = __shfl_xor(id, o);
+          s = fmaxf(fmaxf(s, os), fminf(b, ob));
+          id = ob > b ? oid : id;
+          b = fmaxf(b, ob);
+        }
+        const int64_t row = row0 + 16 * (wave * kF + f) + l16;
+        if (q == 0 && row < n) records[(int64_t)blockIdx.y * n + row] = Mx4Record{b, s, id};
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------- rows of any length
 // kCollect: the instances are those of list (counts->listed of them); the groups whose maximum reaches an instance's threshold are appended to its
 // list.  Otherwise one record per instance, share of the nodes (blockIdx.y) and half of the wavefronts.
 template <bool kCollect>
@@ -261,16 +444,17 @@ __global__ __launch_bounds__(512) void k_mx4_search(Mx4Operand x, Mx4Operand w, 
 }
 
 // What two scores of an instance may differ by in fp32 without being in order: twice the error of one.  steps + 1 roundings of sums of terms whose
-// magnitudes add up to |x| |w| + |w|^2 / 2 at most, |x| taken as what its largest scale allows; a term below the smallest normal fp32
-// number may be lost.  Infinite where the scores could overflow.
-__device__ __forceinline__ double mx4_margin(int exponent, float wmax2, int blocks) {
-  const double x = 6.0 * sqrt(32.0 * blocks) * mx4_pow2(exponent - 127), w = sqrt((double)wmax2);
-  const double size = x * w + 0.5 * (double)wmax2;
+// magnitudes add up to |x| |w| + |w|^2 / 2 at most, |x|^2 taken as what its scales allow (x2: the sum of their squares); a term below the
+// smallest normal fp32 number may be lost.  Infinite where the scores could overflow.
+__device__ __forceinline__ double mx4_margin(double x2, float wmax2, int blocks) {
+  const double size = sqrt(36.0 * 32.0 * x2) * sqrt((double)wmax2) + 0.5 * (double)wmax2;
   if (!(size < 1e37)) return INFINITY;
   return 2.0 * (((blocks + 3) / 4 + 1) * kMx4Delta * size + 1e-34 * blocks);
 }
 
-// 16 instances a wavefront, lane l: instance l % 16.
+// 16 instances a wavefront, lane l: instance l % 16; kMx4Batch of them at a time have the nodes of their groups fetched.  Bound by those loads (16 rows of
+// 64 bytes for one instruction, from L2).
+constexpr int kMx4Batch = 4;
 __global__ __launch_bounds__(256) void k_mx4_resolve(Mx4Rows x, Mx4Rows w, const float *__restrict__ init, int blocks,
                                                      const Mx4Record *__restrict__ records, int shares, const float *__restrict__ parts,
                                                      int nparts, Mx4Counts *__restrict__ counts, int *__restrict__ list,
@@ -295,33 +479,49 @@ __global__ __launch_bounds__(256) void k_mx4_resolve(Mx4Rows x, Mx4Rows w, const
     group = r.best > best ? r.group : group;
     best = fmaxf(best, r.best);
   }
-  mx_f32x4 mine = {0.f, 0.f, 0.f, 0.f};       // scores of nodes 16 group + 4 q ..
-  int exponent = 0;
-  mx_f32x4 acc[16];
-#pragma unroll
-  for (int r = 0; r < 16; ++r) acc[r] = *reinterpret_cast<const mx_f32x4 *>(init + 16 * (int64_t)__builtin_amdgcn_readlane(group, r) + 4 * q);
   const i32x4 none = {0, 0, 0, 0};
-  for (int b0 = 0; b0 < blocks; b0 += 4) {
-    const int b = b0 + q;
-    const bool in = b < blocks;
-    const i32x4 xc = in ? *reinterpret_cast<const i32x4 *>(x.codes + (xr * blocks + b) * 16) : none;
-    const int xs = in ? x.scales[xr * blocks + b] : 0;
-    exponent = max(exponent, xs);
+  mx_f32x4 mine = {0.f, 0.f, 0.f, 0.f};       // scores of nodes 16 group + 4 q ..
+  double x2 = 0.0;
+  bool nan = false;
+#pragma unroll 1
+  for (int r0 = 0; r0 < 16; r0 += kMx4Batch) {
+    mx_f32x4 acc[kMx4Batch];
+    const uint8_t *wc[kMx4Batch], *ws[kMx4Batch];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      int64_t node = 16 * (int64_t)__builtin_amdgcn_readlane(group, r) + l16;
-      if (node >= w.n) node = w.n - 1;
-      const i32x4 wc = in ? *reinterpret_cast<const i32x4 *>(w.codes + (node * blocks + b) * 16) : none;
-      const int ws = in ? w.scales[node * blocks + b] : 0;
-      acc[r] = mx4_mfma<0, 0>(wc, xc, acc[r], ws, xs);
+    for (int r = 0; r < kMx4Batch; ++r) {
+      const int64_t first = 16 * (int64_t)__shfl(group, r0 + r);
+      acc[r] = *reinterpret_cast<const mx_f32x4 *>(init + first + 4 * q);
+      const int64_t node = first + l16 < w.n ? first + l16 : w.n - 1;
+      wc[r] = w.codes + (node * blocks + q) * 16;
+      ws[r] = w.scales + node * blocks + q;
     }
-  }
+    for (int b0 = 0; b0 < blocks; b0 += 4) {
+      const bool in = b0 + q < blocks;
+      const i32x4 xc = in ? *reinterpret_cast<const i32x4 *>(x.codes + (xr * blocks + b0 + q) * 16) : none;
+      const int xs = in ? x.scales[xr * blocks + b0 + q] : 0;
+      if (r0 == 0 && in) {
+        x2 += mx4_pow2(2 * xs - 254);
+        nan |= xs == 255;
+      }
+      i32x4 c[kMx4Batch];
+      int e[kMx4Batch];
 #pragma unroll
-  for (int r = 0; r < 16; ++r)
-    if (l16 == r) mine = acc[r];
-  exponent = max(exponent, __shfl_xor(exponent, 16));
-  exponent = max(exponent, __shfl_xor(exponent, 32));
-  const double margin = mx4_margin(exponent, wmax2, blocks);
+      for (int r = 0; r < kMx4Batch; ++r) {
+        c[r] = in ? *reinterpret_cast<const i32x4 *>(wc[r] + b0 * 16) : none;
+        e[r] = in ? ws[r][b0] : 0;
+      }
+#pragma unroll
+      for (int r = 0; r < kMx4Batch; ++r) acc[r] = mx4_mfma<0, 0>(c[r], xc, acc[r], e[r], xs);
+    }
+#pragma unroll
+    for (int r = 0; r < kMx4Batch; ++r)
+      if (l16 == r0 + r) mine = acc[r];
+  }
+  x2 += __shfl_xor(x2, 16);
+  x2 += __shfl_xor(x2, 32);
+  nan |= __shfl_xor((int)nan, 16) != 0;
+  nan |= __shfl_xor((int)nan, 32) != 0;
+  const double margin = mx4_margin(x2, wmax2, blocks);
   const float reach = __double2float_rd((double)best - margin);
   int near = 0, first = 0x7fffffff;
 #pragma unroll
@@ -333,7 +533,7 @@ __global__ __launch_bounds__(256) void k_mx4_resolve(Mx4Rows x, Mx4Rows w, const
     first = min(first, __shfl_xor(first, o));
   }
   if (q != 0 || row >= x.n) return;
-  if (exponent == 255) {                       // no finite distance to any node
+  if (nan) {                                   // no finite distance to any node
     bmus[row] = 0;
   } else if (!(margin < INFINITY) || !(best > kMx4Lowest)) {
     const int64_t slot = x.n - 1 - atomicAdd(&counts->single, 1);
@@ -354,13 +554,13 @@ __global__ __launch_bounds__(256) void k_mx4_resolve(Mx4Rows x, Mx4Rows w, const
   }
 }
 
-// 16 lanes an instance, one node of a group each.
+// A wavefront an instance: lane l has node l % 16 of a group and every fourth block.
 __global__ __launch_bounds__(256) void k_mx4_exact(Mx4Rows x, Mx4Rows w, int blocks, const Mx4Counts *__restrict__ counts,
                                                    const int *__restrict__ list, const int *__restrict__ found,
                                                    const int *__restrict__ groups, int32_t *__restrict__ bmus) {
-  const int l16 = threadIdx.x & 15;
+  const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
   const int64_t listed = counts->listed, total = listed + counts->single;
-  for (int64_t u = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); u < total; u += (int64_t)gridDim.x * 16) {
+  for (int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); u < total; u += (int64_t)gridDim.x * 4) {
     const int64_t slot = u < listed ? u : x.n - 1 - (u - listed);
     const int64_t row = list[slot];
     const bool all = found[slot] > kMx4List;
@@ -368,18 +568,19 @@ __global__ __launch_bounds__(256) void k_mx4_exact(Mx4Rows x, Mx4Rows w, int blo
     double best = -INFINITY;
     int arg = 0x7fffffff;
     for (int64_t g = 0; g < ng; ++g) {
-      const int64_t node = 16 * (all ? g : (int64_t)groups[slot * kMx4List + g]) + l16;
-      if (node >= w.n) continue;
+      const int64_t node = 16 * (all ? g : (int64_t)groups[slot * kMx4List + g]) + l16, wr = node < w.n ? node : w.n - 1;
       double s = 0.0;
-      for (int b = 0; b < blocks; ++b) {
-        const int ex = x.scales[row * blocks + b], ew = w.scales[node * blocks + b];
+      for (int b = q; b < blocks; b += 4) {
+        const int ex = x.scales[row * blocks + b], ew = w.scales[wr * blocks + b];
         float xw, ww;
         mx4_block_dots(*reinterpret_cast<const i32x4 *>(x.codes + (row * blocks + b) * 16),
-                       *reinterpret_cast<const i32x4 *>(w.codes + (node * blocks + b) * 16), xw, ww);
+                       *reinterpret_cast<const i32x4 *>(w.codes + (wr * blocks + b) * 16), xw, ww);
         s += (double)xw * mx4_pow2(ex + ew - 254) - (double)ww * mx4_pow2(2 * ew - 255);
         if (ex == 255 || ew == 255) s = NAN;
       }
-      if (mx4_better(s, (int)node, best, arg)) { best = s; arg = (int)node; }
+      s += __shfl_xor(s, 16);
+      s += __shfl_xor(s, 32);
+      if (node < w.n && mx4_better(s, (int)node, best, arg)) { best = s; arg = (int)node; }
     }
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) {
@@ -387,24 +588,56 @@ __global__ __launch_bounds__(256) void k_mx4_exact(Mx4Rows x, Mx4Rows w, int blo
       const int i = __shfl_xor(arg, o);
       if (mx4_better(s, i, best, arg)) { best = s; arg = i; }
     }
-    if (l16 == 0) bmus[row] = arg == 0x7fffffff ? 0 : arg;
+    if (lane == 0) bmus[row] = arg == 0x7fffffff ? 0 : arg;
   }
 }
 
-// Shares of the node tiles: the fewest rounds of workgroups (one a CU) times what each of them takes.
-static int sweep_shares(const som_ctx *c, int64_t n) {
-  const int64_t tiles = ((int64_t)c->k + Mx4Sweep::kRowsA - 1) / Mx4Sweep::kRowsA, nb = (n + Mx4Sweep::kRowsB - 1) / Mx4Sweep::kRowsB;
-  const int64_t steps = (mx4_blocks(c->dim) + 3) / 4;
-  int64_t best = 0;
-  int shares = 1;
-  for (int s = 1; s <= tiles && s <= 64; ++s) {
-    const int64_t rounds = (nb * s + c->n_cu - 1) / c->n_cu, cost = rounds * ((tiles + s - 1) / s * steps + 3);
-    if (s == 1 || cost < best) {
-      best = cost;
-      shares = s;
+// How the matrix cores' passes are laid out: instances a workgroup takes, stages or tiles of nodes, shares of those, records of an instance.
+struct Mx4Layout {
+  bool sweep;              // k_mx4_sweep, else k_mx4_search
+  int rows, shares, records;
+  int64_t stages, padded;  // padded: nodes rounded up to whole stages
+};
+
+template <int kT>
+static void sweep_shape(int steps, int *rows, int *nodes, int *cost) {
+  if (steps == kT) {
+    typedef typename Mx4ShapeOf<kT>::type Shape;
+    *rows = Shape::rows;
+    *nodes = 64 * Shape::units;
+    *cost = Shape::units * Shape::F * kT;
+  }
+}
+
+// The shares are those with the fewest rounds of workgroups times what one takes: its stages, and its instances' loads.
+static Mx4Layout search_layout(const som_ctx *c, int64_t n) {
+  Mx4Layout l;
+  const int steps = (mx4_blocks(c->dim) + 3) / 4;
+  int nodes = Mx4Sweep::kRowsA, cost = 0;
+  l.sweep = steps <= kMx4SweepSteps;
+  l.rows = Mx4Sweep::kRowsB;
+  if (l.sweep) {
+    sweep_shape<1>(steps, &l.rows, &nodes, &cost); sweep_shape<2>(steps, &l.rows, &nodes, &cost);
+    sweep_shape<3>(steps, &l.rows, &nodes, &cost); sweep_shape<4>(steps, &l.rows, &nodes, &cost);
+    sweep_shape<5>(steps, &l.rows, &nodes, &cost); sweep_shape<6>(steps, &l.rows, &nodes, &cost);
+    sweep_shape<7>(steps, &l.rows, &nodes, &cost); sweep_shape<8>(steps, &l.rows, &nodes, &cost);
+  } else {
+    cost = 32 * steps;
+  }
+  l.stages = ((int64_t)c->k + nodes - 1) / nodes;
+  l.padded = l.stages * nodes;
+  const int64_t nb = (n + l.rows - 1) / l.rows, at_once = (l.sweep ? 2 : 1) * (int64_t)c->n_cu;
+  int64_t least = 0;
+  l.shares = 1;
+  for (int s = 1; s <= l.stages && s <= 64; ++s) {
+    const int64_t rounds = (nb * s + at_once - 1) / at_once, total = rounds * ((l.stages + s - 1) / s * cost + 64);
+    if (s == 1 || total < least) {
+      least = total;
+      l.shares = s;
     }
   }
-  return shares;
+  l.records = l.shares * (l.sweep ? 1 : Mx4Sweep::kWavesA);
+  return l;
 }
 
 // A direct search takes the vector units about 60 operations for 32 multiply-adds, and two launches; the other five.
@@ -414,16 +647,16 @@ static bool direct_pays(const som_ctx *c, int64_t n) {
 
 struct Mx4SearchScratch {
   float *init, *parts, *threshold;
+  char *stream;
   int *packed_w, *packed_x, *list, *found, *groups;
   Mx4Counts *counts;
   Mx4Record *records;
   size_t bytes;
 };
 
-static Mx4SearchScratch search_scratch(const som_ctx *c, int64_t n, void *base) {
-  const int blocks = mx4_blocks(c->dim);
+static Mx4SearchScratch search_scratch(const som_ctx *c, int64_t n, const Mx4Layout &l, void *base) {
+  const int blocks = mx4_blocks(c->dim), steps = (blocks + 3) / 4;
   const size_t N = (size_t)n;
-  const size_t padded = ((size_t)c->k + Mx4Sweep::kRowsA - 1) / Mx4Sweep::kRowsA * Mx4Sweep::kRowsA;
   Mx4SearchScratch m;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -431,12 +664,13 @@ static Mx4SearchScratch search_scratch(const som_ctx *c, int64_t n, void *base) 
     at += (bytes + 255) / 256 * 256;
     return p;
   };
-  m.init = static_cast<float *>(take(padded * 4));
+  m.init = static_cast<float *>(take((size_t)l.padded * 4));
   m.parts = static_cast<float *>(take(kMx4NodeBlocks * 4));
   m.counts = static_cast<Mx4Counts *>(take(sizeof(Mx4Counts)));
-  m.packed_w = static_cast<int *>(take(mx4_packed_bytes(c->k, blocks)));
-  m.packed_x = static_cast<int *>(take(mx4_packed_bytes(n, blocks)));
-  m.records = static_cast<Mx4Record *>(take((size_t)sweep_shares(c, n) * Mx4Sweep::kWavesA * N * sizeof(Mx4Record)));
+  m.stream = static_cast<char *>(take(l.sweep ? (size_t)(l.padded / 64) * mx4_stream_bytes(steps) : 0));
+  m.packed_w = static_cast<int *>(take(l.sweep ? 0 : mx4_packed_bytes(c->k, blocks)));
+  m.packed_x = static_cast<int *>(take(l.sweep ? 0 : mx4_packed_bytes(n, blocks)));
+  m.records = static_cast<Mx4Record *>(take((size_t)l.records * N * sizeof(Mx4Record)));
   m.list = static_cast<int *>(take(N * 4));
   m.threshold = static_cast<float *>(take(N * 4));
   m.found = static_cast<int *>(take(N * 4));
@@ -446,33 +680,64 @@ static Mx4SearchScratch search_scratch(const som_ctx *c, int64_t n, void *base) 
 }
 
 size_t mx4_search_bytes(const som_ctx *c, int64_t n) {
-  if (!direct_pays(c, n)) return search_scratch(c, n, nullptr).bytes;
+  if (!direct_pays(c, n)) return search_scratch(c, n, search_layout(c, n), nullptr).bytes;
   const int shares = direct_shares(c, n, 1 << direct_lanes_log(mx4_blocks(c->dim)));
   return shares > 1 ? (size_t)n * shares * sizeof(Mx4Best) : 0;
 }
 
+template <int kT, bool kCollect>
+static void launch_sweep(som_ctx *c, Mx4Rows x, const Mx4Layout &l, const Mx4SearchScratch &m, dim3 grid) {
+  hipLaunchKernelGGL((k_mx4_sweep<kT, kCollect>), grid, dim3(256), 0, c->stream, x, mx4_blocks(c->dim), m.stream, l.padded / 64, m.records,
+                     m.counts, m.list, m.threshold, m.found, m.groups);
+}
+
+// The pass over all instances (kCollect: over those that are listed, as many workgroups as fill the chip at most).
+template <bool kCollect>
+static hipError_t launch_pass(som_ctx *c, Mx4Rows x, Mx4Rows w, const Mx4Layout &l, const Mx4SearchScratch &m) {
+  const int blocks = mx4_blocks(c->dim);
+  const int64_t nb = (x.n + l.rows - 1) / l.rows;
+  dim3 grid((unsigned)nb, l.shares);
+  if (kCollect) {
+    const unsigned ways = (unsigned)(l.stages < 16 ? l.stages : 16), most = 2 * c->n_cu / ways;
+    grid = dim3((unsigned)(nb < most ? nb : most), ways);
+  }
+  if (l.sweep) {
+    switch ((blocks + 3) / 4) {
+      case 1: launch_sweep<1, kCollect>(c, x, l, m, grid); break;
+      case 2: launch_sweep<2, kCollect>(c, x, l, m, grid); break;
+      case 3: launch_sweep<3, kCollect>(c, x, l, m, grid); break;
+      case 4: launch_sweep<4, kCollect>(c, x, l, m, grid); break;
+      case 5: launch_sweep<5, kCollect>(c, x, l, m, grid); break;
+      case 6: launch_sweep<6, kCollect>(c, x, l, m, grid); break;
+      case 7: launch_sweep<7, kCollect>(c, x, l, m, grid); break;
+      default: launch_sweep<8, kCollect>(c, x, l, m, grid);
+    }
+    return hipGetLastError();
+  }
+  const hipError_t e = launch_mx4_pack_scales(c->stream, x.scales, x.n, blocks, false, m.packed_x, kCollect ? m.list : nullptr,
+                                              kCollect ? &m.counts->listed : nullptr);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(k_mx4_search<kCollect>, grid, dim3(Mx4Sweep::kThreads), 0, c->stream, Mx4Operand{x, m.packed_x}, Mx4Operand{w, m.packed_w},
+                     m.init, blocks, c->zero16, l.stages, m.records, m.counts, m.list, m.threshold, m.found, m.groups);
+  return hipGetLastError();
+}
+
 hipError_t launch_bmu_mx4(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int32_t *bmus) {
   if (direct_pays(c, x.n)) return search_direct(c, x, w, scratch, bmus);
-  const Mx4SearchScratch m = search_scratch(c, x.n, scratch);
+  const Mx4Layout l = search_layout(c, x.n);
+  const Mx4SearchScratch m = search_scratch(c, x.n, l, scratch);
   const int blocks = mx4_blocks(c->dim);
-  const int64_t tiles = (w.n + Mx4Sweep::kRowsA - 1) / Mx4Sweep::kRowsA, padded = tiles * Mx4Sweep::kRowsA;
-  const int parts = padded / 64 < kMx4NodeBlocks ? (int)(padded / 64) : kMx4NodeBlocks, shares = sweep_shares(c, x.n);
-  hipLaunchKernelGGL(k_mx4_nodes, dim3(parts), dim3(256), 0, c->stream, w, blocks, padded, m.init, m.packed_w, m.parts, m.counts);
-  hipError_t e = launch_mx4_pack_scales(c->stream, x.scales, x.n, blocks, false, m.packed_x);
+  const int parts = l.padded / 64 < kMx4NodeBlocks ? (int)(l.padded / 64) : kMx4NodeBlocks;
+  if (l.sweep) hipLaunchKernelGGL(k_mx4_nodes<true>, dim3(parts), dim3(256), 0, c->stream, w, blocks, l.padded, m.init, m.stream, m.packed_w, m.parts, m.counts);
+  else hipLaunchKernelGGL(k_mx4_nodes<false>, dim3(parts), dim3(256), 0, c->stream, w, blocks, l.padded, m.init, m.stream, m.packed_w, m.parts, m.counts);
+  hipError_t e = launch_pass<false>(c, x, w, l, m);
   if (e != hipSuccess) return e;
-  const Mx4Operand ox = {x, m.packed_x}, ow = {w, m.packed_w};
-  hipLaunchKernelGGL(k_mx4_search<false>, dim3((unsigned)((x.n + Mx4Sweep::kRowsB - 1) / Mx4Sweep::kRowsB), shares), dim3(Mx4Sweep::kThreads), 0,
-                     c->stream, ox, ow, m.init, blocks, c->zero16, tiles, m.records, m.counts, m.list, m.threshold, m.found, m.groups);
-  hipLaunchKernelGGL(k_mx4_resolve, dim3((unsigned)((x.n + 63) / 64)), dim3(256), 0, c->stream, x, w, m.init, blocks, m.records,
-                     shares * Mx4Sweep::kWavesA, m.parts, parts, m.counts, m.list, m.threshold, m.found, m.groups, bmus);
-  e = launch_mx4_pack_scales(c->stream, x.scales, x.n, blocks, false, m.packed_x, m.list, &m.counts->listed);
+  hipLaunchKernelGGL(k_mx4_resolve, dim3((unsigned)((x.n + 63) / 64)), dim3(256), 0, c->stream, x, w, m.init, blocks, m.records, l.records,
+                     m.parts, parts, m.counts, m.list, m.threshold, m.found, m.groups, bmus);
+  e = launch_pass<true>(c, x, w, l, m);
   if (e != hipSuccess) return e;
-  const int64_t most = (x.n + Mx4Sweep::kRowsB - 1) / Mx4Sweep::kRowsB;
-  const unsigned ways = (unsigned)(tiles < 16 ? tiles : 16), wide = (unsigned)(most < 2 * c->n_cu / ways ? most : 2 * c->n_cu / ways);
-  hipLaunchKernelGGL(k_mx4_search<true>, dim3(wide < 1 ? 1 : wide, ways), dim3(Mx4Sweep::kThreads), 0, c->stream, ox, ow, m.init, blocks,
-                     c->zero16, tiles, m.records, m.counts, m.list, m.threshold, m.found, m.groups);
-  const int64_t rows16 = (x.n + 15) / 16;
-  hipLaunchKernelGGL(k_mx4_exact, dim3((unsigned)(rows16 < 8 * c->n_cu ? rows16 : 8 * c->n_cu)), dim3(256), 0, c->stream, x, w, blocks, m.counts,
+  const int64_t most = (x.n + 3) / 4;
+  hipLaunchKernelGGL(k_mx4_exact, dim3((unsigned)(most < 8 * c->n_cu ? most : 8 * c->n_cu)), dim3(256), 0, c->stream, x, w, blocks, m.counts,
                      m.list, m.found, m.groups, bmus);
   return hipGetLastError();
 }
