@@ -199,27 +199,35 @@ __global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int64_
 }
 
 // ---------------------------------------------------------------- rows of up to 8 steps (1,024 features)
-// The instances stay in registers, the nodes stream through LDS.  A wavefront has 16 kF instances; per 64 nodes (one unit of the stream) it reads 4 kT
-// fragments for 4 kT kF instructions.  Results of four instructions are a lane's 16 scores of one instance: eight v_max3, and four operations
-// for the running maximum, its place and the runner-up, 12 to 4 kT instructions of 16 cycles, which one wavefront would issue in the same
-// time if kT = 1; so with few steps the instances are taken one fragment after the other, the maxima of one between the products of the next.
-// Two stages in LDS of kUnits units each: the loads of a stage are issued when the one before it begins.
-template <int kT, int kF, int kUnits, bool kByF>
+// The instances stay in registers, the nodes stream through LDS.  A wavefront has 16 kF instances; for a step of 64 nodes (a piece) it
+// reads four fragments for 4 kF instructions of 16 cycles.  The results of four instructions are a lane's 16 scores of one
+// instance: eight v_max3, and four operations for the running maximum, its place and the runner-up - in the issue slots between the
+// products of the next 64 nodes (kT = 1: of the next instances; there the 12 operations to four instructions take as many slots as there are).
+// The compiler keeps reads, products and maxima apart unless the order is fixed, as it is here.  Two stages in LDS of kUnits times 64 nodes: a
+// piece is read into registers while the one before it is multiplied, so when the last of a stage begins the stage is free and gets the
+// loads of the one after the next.
+template <int kT, int kF, int kUnits>
 struct Mx4SweepShape {
-  static constexpr int T = kT, F = kF, units = kUnits, rows = 64 * kF;
-  static constexpr bool by_f = kByF;
+  static constexpr int F = kF, units = kUnits, rows = 64 * kF;
   static constexpr int unit = mx4_stream_bytes(kT), stage = kUnits * unit, chunks = stage / 1024, lds = 2 * stage;
 };
+// F: as many as two wavefronts a SIMD leave registers for.
 template <int kT> struct Mx4ShapeOf;
-template <> struct Mx4ShapeOf<1> { typedef Mx4SweepShape<1, 8, 4, true> type; };
-template <> struct Mx4ShapeOf<2> { typedef Mx4SweepShape<2, 8, 2, true> type; };
-template <> struct Mx4ShapeOf<3> { typedef Mx4SweepShape<3, 4, 2, true> type; };
-template <> struct Mx4ShapeOf<4> { typedef Mx4SweepShape<4, 4, 1, false> type; };
-template <> struct Mx4ShapeOf<5> { typedef Mx4SweepShape<5, 4, 1, false> type; };
-template <> struct Mx4ShapeOf<6> { typedef Mx4SweepShape<6, 4, 1, false> type; };
-template <> struct Mx4ShapeOf<7> { typedef Mx4SweepShape<7, 3, 1, false> type; };
-template <> struct Mx4ShapeOf<8> { typedef Mx4SweepShape<8, 3, 1, false> type; };
+template <> struct Mx4ShapeOf<1> { typedef Mx4SweepShape<1, 8, 4> type; };
+template <> struct Mx4ShapeOf<2> { typedef Mx4SweepShape<2, 6, 2> type; };
+template <> struct Mx4ShapeOf<3> { typedef Mx4SweepShape<3, 5, 2> type; };
+template <> struct Mx4ShapeOf<4> { typedef Mx4SweepShape<4, 4, 1> type; };
+template <> struct Mx4ShapeOf<5> { typedef Mx4SweepShape<5, 4, 1> type; };
+template <> struct Mx4ShapeOf<6> { typedef Mx4SweepShape<6, 4, 1> type; };
+template <> struct Mx4ShapeOf<7> { typedef Mx4SweepShape<7, 3, 1> type; };
+template <> struct Mx4ShapeOf<8> { typedef Mx4SweepShape<8, 3, 1> type; };
 constexpr int kMx4SweepSteps = 8;
+
+// Nothing moves across: neither the loads (the assembly) nor anything else (the barrier of the scheduler).
+__device__ __forceinline__ void mx4_in_order() {
+  asm volatile("" : : : "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
 
 // kCollect as in k_mx4_search.
 template <int kT, bool kCollect>
@@ -229,24 +237,38 @@ __global__ __launch_bounds__(256, 2) void k_mx4_sweep(Mx4Rows x, int blocks, con
                                                       int *__restrict__ found, int *__restrict__ groups) {
   typedef typename Mx4ShapeOf<kT>::type Shape;
   constexpr int kF = Shape::F, kUnits = Shape::units;
+  constexpr bool kByF = kT == 1;
   __shared__ __attribute__((aligned(16))) char smem[Shape::lds];
   const unsigned lds = (unsigned)(size_t)(mx4_lds_t)smem;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, q = lane >> 4;
   const int64_t n = kCollect ? counts->listed : x.n;
   // stages of the stream: this share's
-  const int64_t all = (all_units + kUnits - 1) / kUnits, per = (all + gridDim.y - 1) / gridDim.y, first = blockIdx.y * per;
+  const int64_t all = all_units / kUnits, per = (all + gridDim.y - 1) / gridDim.y, first = blockIdx.y * per;
   const int64_t last = first + per < all ? first + per : all;
   if (first >= last) return;
-  auto load = [&](int64_t at, int half) {
-    const char *src = stream + at * Shape::stage + lane * 16;
+  auto load = [&](int64_t at, int half) {      // (past the share: its last stage again, which nobody reads)
+    const char *src = stream + (at < last ? at : last - 1) * Shape::stage;
 #pragma unroll
     for (int u = 0; u < (Shape::chunks + 3) / 4; ++u) {
-      const int c = 4 * u + wave;
-      if (c < Shape::chunks) mx4_load_to_lds(src + c * 1024, lds + half * Shape::stage + c * 1024);
+      int c = 4 * u + wave;                    // (no branch, which would tear the order below apart: the last chunk more than once)
+      if (Shape::chunks % 4 != 0 && c >= Shape::chunks) c = Shape::chunks - 1;
+      mx4_load_to_lds_at(src + c * 1024, lane * 16, lds + half * Shape::stage + c * 1024);
     }
+  };
+  struct Piece {
+    i32x4 w[4];
+    int sw;
+    mx_f32x4 from[4];
+  };
+  // one of the reads of a piece: the step's fragments and scales, what the accumulators start from
+  auto read = [&](Piece &p, const char *unit, int s, int i) {
+    if (i < 4) p.w[i] = *reinterpret_cast<const i32x4 *>(unit + (s * 4 + i) * 1024 + lane * 16);
+    else if (i == 4) p.sw = *reinterpret_cast<const int *>(unit + kT * 4096 + s * 256 + lane * 4);
+    else if (i < 9 && s == 0) p.from[i - 5] = *reinterpret_cast<const mx_f32x4 *>(unit + kT * 4352 + (16 * q + 4 * (i - 5)) * 4);
   };
   for (int64_t row0 = (int64_t)blockIdx.x * Shape::rows; row0 < n; row0 += (int64_t)gridDim.x * Shape::rows) {
     load(first, 0);
+    load(first + 1, 1);
     i32x4 y[kF][kT];
     int sy[(kF + 3) / 4][kT];
     float best[kF], second[kF];
@@ -268,80 +290,79 @@ __global__ __launch_bounds__(256, 2) void k_mx4_sweep(Mx4Rows x, int blocks, con
       second[f] = kMx4Lowest;
       at[f] = 0;
     }
-    // scores a of instance fragment f and nodes 64 unit + 16 q .. + 15
-    auto maxima = [&](const mx_f32x4 (&a)[4], int f, int unit) {
-      float m = kMx4Lowest;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        m = fmaxf(fmaxf(m, a[t][0]), a[t][1]);
-        m = fmaxf(fmaxf(m, a[t][2]), a[t][3]);
-      }
-      if (kCollect) {
-        if (m >= best[f]) {
-          const int64_t slot = row0 + 16 * (wave * kF + f) + l16;
-          const int place = atomicAdd(&found[slot], 1);
-          if (place < kMx4List) groups[slot * kMx4List + place] = 4 * unit + q;
-        }
-      } else {
-        second[f] = __builtin_amdgcn_fmed3f(second[f], best[f], m);
-        at[f] = m > best[f] ? unit : at[f];
-        best[f] = fmaxf(best[f], m);
+    // Scores a of instance fragment f and nodes 64 unit + 16 q .. + 15, a quarter of the work at a time.
+    float m = kMx4Lowest;
+    bool larger = false;
+    auto maxima = [&](const mx_f32x4 (&a)[4], int f, int unit, int part) {
+      if (part == 0) {
+        m = fmaxf(fmaxf(kMx4Lowest, a[0][0]), a[0][1]);
+        m = fmaxf(fmaxf(m, a[0][2]), a[0][3]);
+        m = fmaxf(fmaxf(m, a[1][0]), a[1][1]);
+      } else if (part == 1) {
+        m = fmaxf(fmaxf(m, a[1][2]), a[1][3]);
+        m = fmaxf(fmaxf(m, a[2][0]), a[2][1]);
+        m = fmaxf(fmaxf(m, a[2][2]), a[2][3]);
+      } else if (part == 2) {
+        m = fmaxf(fmaxf(m, a[3][0]), a[3][1]);
+        m = fmaxf(fmaxf(m, a[3][2]), a[3][3]);
+        if (!kCollect) second[f] = __builtin_amdgcn_fmed3f(second[f], best[f], m);
+      } else if (!kCollect) {
+        larger = m > best[f];
+        at[f] = larger ? unit : at[f];
+        best[f] = larger ? m : best[f];
+      } else if (m >= best[f]) {
+        const int64_t slot = row0 + 16 * (wave * kF + f) + l16;
+        const int place = atomicAdd(&found[slot], 1);
+        if (place < kMx4List) groups[slot * kMx4List + place] = 4 * unit + q;
       }
     };
-    mx_f32x4 held[2][4];                       // kByF: scores whose maxima are still to be taken, of fragment kF - 1
+    // kByF: the scores of two fragments of instances, the last ones' to begin with [1]; else those of all
+    constexpr int kAcc = kByF ? 2 : kF;
+    static_assert(!kByF || kF % 2 == 0, "the last fragment's scores are acc[1]");
+    mx_f32x4 acc[kAcc][4];
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int f = 0; f < kAcc; ++f)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) held[1][t][r] = kMx4Lowest;
-    static_assert(!Shape::by_f || kF % 2 == 0, "the last fragment's scores are held[1]");
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[f][t][r] = kMx4Lowest;
+    mx4_wait<0>();
+    mx4_barrier();
+    Piece now, next;
+#pragma unroll
+    for (int i = 0; i < 9; ++i) read(now, smem, 0, i);
+#pragma unroll 1
     for (int64_t it = first; it < last; ++it) {
       const int half = (int)(it - first) & 1;
-      mx4_wait<0>();
-      mx4_barrier();
-      if (it + 1 < last) load(it + 1, half ^ 1);
-#pragma unroll 1
+      const char *stage = smem + half * Shape::stage, *other = smem + (half ^ 1) * Shape::stage;
+#pragma unroll
       for (int u = 0; u < kUnits; ++u) {
         const int unit = (int)it * kUnits + u;
-        const char *base = smem + half * Shape::stage + u * Shape::unit;
-        mx_f32x4 from[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) from[t] = *reinterpret_cast<const mx_f32x4 *>(base + kT * 4352 + (16 * q + 4 * t) * 4);
-        if (Shape::by_f) {
-          i32x4 w[kT][4];
-          int sw[kT];
-#pragma unroll
-          for (int s = 0; s < kT; ++s) {
-            sw[s] = *reinterpret_cast<const int *>(base + kT * 4096 + s * 256 + lane * 4);
-#pragma unroll
-            for (int t = 0; t < 4; ++t) w[s][t] = *reinterpret_cast<const i32x4 *>(base + (s * 4 + t) * 1024 + lane * 16);
+        for (int s = 0; s < kT; ++s) {
+          if (u == kUnits - 1 && s == kT - 1) {
+            mx4_wait<0>();                     // everybody has read this stage, and the other one is there
+            mx4_barrier();
+            load(it + 2, half);
           }
+          const char *from = s + 1 < kT ? stage + u * Shape::unit : u + 1 < kUnits ? stage + (u + 1) * Shape::unit : other;
 #pragma unroll
-          for (int f = 0; f < kF; ++f) {
-#pragma unroll
-            for (int s = 0; s < kT; ++s)
-#pragma unroll
-              for (int t = 0; t < 4; ++t)
-                held[f & 1][t] = mx4_mfma_at(t, f & 3, w[s][t], y[f][s], s == 0 ? from[t] : held[f & 1][t], sw[s], sy[f / 4][s]);
-            maxima(held[(f & 1) ^ 1], f == 0 ? kF - 1 : f - 1, f == 0 ? unit - 1 : unit);
-          }
-        } else {
-          mx_f32x4 acc[kF][4];
-#pragma unroll
-          for (int s = 0; s < kT; ++s) {
-            const int sw = *reinterpret_cast<const int *>(base + kT * 4096 + s * 256 + lane * 4);
+          for (int f = 0; f < kF; ++f)
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-              const i32x4 w = *reinterpret_cast<const i32x4 *>(base + (s * 4 + t) * 1024 + lane * 16);
-#pragma unroll
-              for (int f = 0; f < kF; ++f) acc[f][t] = mx4_mfma_at(t, f & 3, w, y[f][s], s == 0 ? from[t] : acc[f][t], sw, sy[f / 4][s]);
+              mx_f32x4 &to = acc[kByF ? f & 1 : f][t];
+              to = mx4_mfma_at(t, f & 3, now.w[t], y[f][s], s == 0 ? now.from[t] : to, now.sw, sy[f / 4][s]);
+              if (4 * f + t < 9) read(next, from, s + 1 < kT ? s + 1 : 0, 4 * f + t);
+              if (s == 0 && f == 0) maxima(acc[kAcc - 1], kF - 1, unit - 1, t);
+              else if (s == kT - 1 && f > 0) maxima(acc[kByF ? (f & 1) ^ 1 : f - 1], f - 1, unit, t);
+              mx4_in_order();
             }
-          }
-#pragma unroll
-          for (int f = 0; f < kF; ++f) maxima(acc[f], f, unit);
+          now = next;
         }
       }
     }
-    if (Shape::by_f) maxima(held[1], kF - 1, (int)last * kUnits - 1);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) maxima(acc[kAcc - 1], kF - 1, (int)last * kUnits - 1, t);
     mx4_wait<0>();
     mx4_barrier();                             // the stages may be filled again
     if (!kCollect) {

@@ -23,6 +23,10 @@ namespace som {
 __device__ __forceinline__ void mx4_load_to_lds(const void *g, unsigned lds_base) {
   asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(g), "s"(lds_base) : "memory", "m0");
 }
+// The same from base + offset, the base in scalar registers.
+__device__ __forceinline__ void mx4_load_to_lds_at(const void *base, int offset, unsigned lds_base) {
+  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(lds_base) : "memory", "m0");
+}
 #pragma clang diagnostic pop
 
 typedef __attribute__((address_space(3))) void *mx4_lds_t;
