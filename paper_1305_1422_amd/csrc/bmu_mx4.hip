@@ -132,13 +132,12 @@ struct Mx4Record {
   int group;
 };
 
-// Nodes as k_mx4_sweep reads them: 64 at a time, their fragments ([step][4] of 1 KB), per step a word of scales per lane, and what the
-// accumulators start from in the order of the nodes, rounded up to whole KB.
+// The stream of nodes, 64 at a time (a unit): per step and group of 16 nodes their fragment (lane l: block l / 16 of node l % 16; 1 KB), then
+// per step the packed scales (mx4_tiles.hpp), then what the accumulators start from in the order of the nodes, rounded up to whole KB.
 __host__ __device__ constexpr int mx4_stream_bytes(int steps) { return steps * 4096 + ((steps + 1) * 256 + 1023) / 1024 * 1024; }
 
 // A workgroup takes 64 nodes at a time.  parts[blockIdx.x]: the largest |w|^2 it saw (fp64, rounded up to fp32; infinity if it overflows).
-// kStream: the nodes as k_mx4_sweep reads them, else their packed scales.
-template <bool kStream>
+// packed, init: the scales and starting values by themselves for k_mx4_search, or null.
 __global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int64_t padded, float *__restrict__ init, char *__restrict__ stream,
                                                    int *__restrict__ packed, float *__restrict__ parts, Mx4Counts *__restrict__ counts) {
   __shared__ double s_norm[4][64];
@@ -147,7 +146,7 @@ __global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int64_
   if (blockIdx.x == 0 && threadIdx.x == 0) *counts = Mx4Counts{0, 0};
   float most = 0.f;
   for (int64_t g = blockIdx.x; g < padded / 64; g += gridDim.x) {
-    char *mine = kStream ? stream + g * mx4_stream_bytes(steps) : nullptr;
+    char *mine = stream + g * (int64_t)mx4_stream_bytes(steps);
     double norm[4] = {0, 0, 0, 0};
     for (int s = wave; s < steps; s += 4) {
       const int block = 4 * s + q;
@@ -156,21 +155,26 @@ __global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int64_
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         const int64_t node = 64 * g + mx4_dealt(t, i);
-        const bool in = block < blocks && node < w.n;
-        const i32x4 none = {0, 0, 0, 0};
-        x[t] = in ? *reinterpret_cast<const i32x4 *>(w.codes + (node * blocks + block) * 16) : none;
-        v |= (in ? (unsigned)w.scales[node * blocks + block] : 0u) << (8 * t);
+        const int64_t b = (node < w.n ? node : w.n - 1) * blocks + (block < blocks ? block : blocks - 1);
+        x[t] = *reinterpret_cast<const i32x4 *>(w.codes + b * 16);
+        v |= (unsigned)w.scales[b] << (8 * t);
       }
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (block >= blocks || 64 * g + mx4_dealt(t, i) >= w.n) {
+          x[t] = i32x4{0, 0, 0, 0};
+          v &= ~(255u << (8 * t));
+        }
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         const int e = (v >> (8 * t)) & 255;
         float xx, ww;
         mx4_block_dots(x[t], x[t], xx, ww);
         norm[t] += e == 255 ? (double)NAN : (double)ww * mx4_pow2(2 * e - 254);
-        if (kStream) *reinterpret_cast<i32x4 *>(mine + (s * 4 + t) * 1024 + lane * 16) = x[t];
+        *reinterpret_cast<i32x4 *>(mine + s * 4096 + (i >> 2) * 1024 + (16 * q + 4 * t + (i & 3)) * 16) = x[t];
       }
-      if (kStream) *reinterpret_cast<unsigned *>(mine + steps * 4096 + s * 256 + lane * 4) = v;
-      else if (64 * g < w.n) packed[(g * steps + s) * 64 + lane] = (int)v;
+      *reinterpret_cast<unsigned *>(mine + steps * 4096 + s * 256 + lane * 4) = v;
+      if (packed && 64 * g < w.n) packed[(g * steps + s) * 64 + lane] = (int)v;
     }
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -184,8 +188,8 @@ __global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int64_
       const int64_t node = 64 * g + threadIdx.x;
       const bool usable = node < w.n && n2 == n2;      // a node with a NaN, and what is past the last one, can never win
       const float from = usable ? (float)(-0.5 * n2) : -INFINITY;
-      init[node] = from;
-      if (kStream) *reinterpret_cast<float *>(mine + steps * 4096 + steps * 256 + threadIdx.x * 4) = from;
+      if (init) init[node] = from;
+      *reinterpret_cast<float *>(mine + steps * 4096 + steps * 256 + threadIdx.x * 4) = from;
       if (usable) most = fmaxf(most, __double2float_ru(n2));
     }
     __syncthreads();
@@ -209,19 +213,29 @@ __global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int64_
 template <int kT, int kF, int kUnits>
 struct Mx4SweepShape {
   static constexpr int F = kF, units = kUnits, rows = 64 * kF;
-  static constexpr int unit = mx4_stream_bytes(kT), stage = kUnits * unit, chunks = stage / 1024, lds = 2 * stage;
+  static constexpr int unit = mx4_stream_bytes(kT), stage = kUnits * unit, rest = unit / 1024 - 4 * kT, lds = 2 * stage;
 };
-// F: as many as two wavefronts a SIMD leave registers for.
-template <int kT> struct Mx4ShapeOf;
-template <> struct Mx4ShapeOf<1> { typedef Mx4SweepShape<1, 8, 4> type; };
-template <> struct Mx4ShapeOf<2> { typedef Mx4SweepShape<2, 6, 2> type; };
-template <> struct Mx4ShapeOf<3> { typedef Mx4SweepShape<3, 5, 2> type; };
-template <> struct Mx4ShapeOf<4> { typedef Mx4SweepShape<4, 4, 1> type; };
-template <> struct Mx4ShapeOf<5> { typedef Mx4SweepShape<5, 4, 1> type; };
-template <> struct Mx4ShapeOf<6> { typedef Mx4SweepShape<6, 4, 1> type; };
-template <> struct Mx4ShapeOf<7> { typedef Mx4SweepShape<7, 3, 1> type; };
-template <> struct Mx4ShapeOf<8> { typedef Mx4SweepShape<8, 3, 1> type; };
+// F: as many as two wavefronts a SIMD leave registers for (one fewer with the lists to write).
+template <int kT, bool kCollect> struct Mx4ShapeOf;
+template <bool kCollect> struct Mx4ShapeOf<1, kCollect> { typedef Mx4SweepShape<1, 8, 4> type; };
+template <bool kCollect> struct Mx4ShapeOf<2, kCollect> { typedef Mx4SweepShape<2, kCollect ? 5 : 6, 2> type; };
+template <bool kCollect> struct Mx4ShapeOf<3, kCollect> { typedef Mx4SweepShape<3, kCollect ? 4 : 5, 2> type; };
+template <bool kCollect> struct Mx4ShapeOf<4, kCollect> { typedef Mx4SweepShape<4, kCollect ? 3 : 4, 1> type; };
+template <bool kCollect> struct Mx4ShapeOf<5, kCollect> { typedef Mx4SweepShape<5, kCollect ? 3 : 4, 1> type; };
+template <bool kCollect> struct Mx4ShapeOf<6, kCollect> { typedef Mx4SweepShape<6, kCollect ? 2 : 4, 1> type; };
+template <bool kCollect> struct Mx4ShapeOf<7, kCollect> { typedef Mx4SweepShape<7, kCollect ? 2 : 3, 1> type; };
+template <bool kCollect> struct Mx4ShapeOf<8, kCollect> { typedef Mx4SweepShape<8, kCollect ? 2 : 3, 1> type; };
 constexpr int kMx4SweepSteps = 8;
+
+// The work of a pass, (block of instances, stage of nodes) pairs in that order, is cut into one piece of `per` stages for every workgroup, so
+// that all of them have the same to do whatever the sizes; a piece may end one block of instances and begin another.
+struct Mx4Cut {
+  int64_t stages, per;     // of a block of instances, of a workgroup
+  int rows;                // instances of a block
+};
+// Records of an instance: those of the workgroups first .. last that have stages of its block.
+__host__ __device__ inline int64_t mx4_first_piece(const Mx4Cut &c, int64_t block) { return block * c.stages / c.per; }
+__host__ __device__ inline int64_t mx4_last_piece(const Mx4Cut &c, int64_t block) { return ((block + 1) * c.stages - 1) / c.per; }
 
 // Nothing moves across: neither the loads (the assembly) nor anything else (the barrier of the scheduler).
 __device__ __forceinline__ void mx4_in_order() {
@@ -231,28 +245,41 @@ __device__ __forceinline__ void mx4_in_order() {
 
 // kCollect as in k_mx4_search.
 template <int kT, bool kCollect>
-__global__ __launch_bounds__(256, 2) void k_mx4_sweep(Mx4Rows x, int blocks, const char *__restrict__ stream, int64_t all_units,
+__global__ __launch_bounds__(256, 2) void k_mx4_sweep(Mx4Rows x, int blocks, const char *__restrict__ stream, Mx4Cut cut,
                                                       Mx4Record *__restrict__ records, const Mx4Counts *__restrict__ counts,
                                                       const int *__restrict__ list, const float *__restrict__ threshold,
                                                       int *__restrict__ found, int *__restrict__ groups) {
-  typedef typename Mx4ShapeOf<kT>::type Shape;
+  typedef typename Mx4ShapeOf<kT, kCollect>::type Shape;
   constexpr int kF = Shape::F, kUnits = Shape::units;
   constexpr bool kByF = kT == 1;
   __shared__ __attribute__((aligned(16))) char smem[Shape::lds];
   const unsigned lds = (unsigned)(size_t)(mx4_lds_t)smem;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, q = lane >> 4;
-  const int64_t n = kCollect ? counts->listed : x.n;
-  // stages of the stream: this share's
-  const int64_t all = all_units / kUnits, per = (all + gridDim.y - 1) / gridDim.y, first = blockIdx.y * per;
-  const int64_t last = first + per < all ? first + per : all;
-  if (first >= last) return;
+  const int64_t n = kCollect ? counts->listed : x.n, nb = (n + Shape::rows - 1) / Shape::rows;
+  if (kCollect) {                              // how many there are is known here only
+    if (n == 0) return;
+    cut.per = (nb * cut.stages + gridDim.x - 1) / gridDim.x;
+  }
+  int64_t pos = blockIdx.x * cut.per;
+  const int64_t end = pos + cut.per < nb * cut.stages ? pos + cut.per : nb * cut.stages;
+  // Wavefront t fetches the fragments t that the products take (mx4_dealt: a quarter of the rows from each group of 16), so that LDS has
+  // them as the reads below want them.
+  const int deal = (l16 >> 2) * 1024 + q * 256 + (l16 & 3) * 16 + wave * 64;
+  int64_t first = 0, last = 0;
   auto load = [&](int64_t at, int half) {      // (past the share: its last stage again, which nobody reads)
     const char *src = stream + (at < last ? at : last - 1) * Shape::stage;
+    const unsigned dst = lds + half * Shape::stage;
 #pragma unroll
-    for (int u = 0; u < (Shape::chunks + 3) / 4; ++u) {
-      int c = 4 * u + wave;                    // (no branch, which would tear the order below apart: the last chunk more than once)
-      if (Shape::chunks % 4 != 0 && c >= Shape::chunks) c = Shape::chunks - 1;
-      mx4_load_to_lds_at(src + c * 1024, lane * 16, lds + half * Shape::stage + c * 1024);
+    for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+      for (int s = 0; s < kT; ++s)
+        mx4_load_to_lds_at(src + u * Shape::unit + s * 4096, deal, dst + u * Shape::unit + (4 * s + wave) * 1024);
+#pragma unroll
+    for (int u = 0; u < (kUnits * Shape::rest + 3) / 4; ++u) {
+      int c = 4 * u + wave;                    // (no branch, which would tear the order below apart: the last one more than once)
+      if ((kUnits * Shape::rest) % 4 != 0 && c >= kUnits * Shape::rest) c = kUnits * Shape::rest - 1;
+      const int off = c / Shape::rest * Shape::unit + kT * 4096 + c % Shape::rest * 1024;
+      mx4_load_to_lds_at(src + off, lane * 16, dst + off);
     }
   };
   struct Piece {
@@ -266,7 +293,11 @@ __global__ __launch_bounds__(256, 2) void k_mx4_sweep(Mx4Rows x, int blocks, con
     else if (i == 4) p.sw = *reinterpret_cast<const int *>(unit + kT * 4096 + s * 256 + lane * 4);
     else if (i < 9 && s == 0) p.from[i - 5] = *reinterpret_cast<const mx_f32x4 *>(unit + kT * 4352 + (16 * q + 4 * (i - 5)) * 4);
   };
-  for (int64_t row0 = (int64_t)blockIdx.x * Shape::rows; row0 < n; row0 += (int64_t)gridDim.x * Shape::rows) {
+  while (pos < end) {
+    const int64_t block = pos / cut.stages, row0 = block * Shape::rows;
+    first = pos - block * cut.stages;
+    last = first + (end - pos) < cut.stages ? first + (end - pos) : cut.stages;
+    pos += last - first;
     load(first, 0);
     load(first + 1, 1);
     i32x4 y[kF][kT];
@@ -280,10 +311,10 @@ __global__ __launch_bounds__(256, 2) void k_mx4_sweep(Mx4Rows x, int blocks, con
       if (kCollect) row = list[row];
 #pragma unroll
       for (int s = 0; s < kT; ++s) {
-        const bool in = 4 * s + q < blocks;
-        const i32x4 none = {0, 0, 0, 0};
-        y[f][s] = in ? *reinterpret_cast<const i32x4 *>(x.codes + (row * blocks + 4 * s + q) * 16) : none;
-        const int e = in ? x.scales[row * blocks + 4 * s + q] : 0;
+        // (what is past the end meets zeros of the stream)
+        const int64_t b = row * blocks + (4 * s + q < blocks ? 4 * s + q : blocks - 1);
+        y[f][s] = *reinterpret_cast<const i32x4 *>(x.codes + b * 16);
+        const int e = x.scales[b];
         sy[f / 4][s] = f % 4 == 0 ? e : sy[f / 4][s] | e << (8 * (f % 4));
       }
       best[f] = kCollect ? (slot < n ? threshold[slot] : INFINITY) : kMx4Lowest;
@@ -352,7 +383,9 @@ __global__ __launch_bounds__(256, 2) void k_mx4_sweep(Mx4Rows x, int blocks, con
             for (int t = 0; t < 4; ++t) {
               mx_f32x4 &to = acc[kByF ? f & 1 : f][t];
               to = mx4_mfma_at(t, f & 3, now.w[t], y[f][s], s == 0 ? now.from[t] : to, now.sw, sy[f / 4][s]);
-              if (4 * f + t < 9) read(next, from, s + 1 < kT ? s + 1 : 0, 4 * f + t);
+              read(next, from, s + 1 < kT ? s + 1 : 0, 4 * f + t);
+              if (f == kF - 1 && t == 3)       // (fewer products than reads)
+                for (int i = 4 * kF; i < 9; ++i) read(next, from, s + 1 < kT ? s + 1 : 0, i);
               if (s == 0 && f == 0) maxima(acc[kAcc - 1], kF - 1, unit - 1, t);
               else if (s == kT - 1 && f > 0) maxima(acc[kByF ? (f & 1) ^ 1 : f - 1], f - 1, unit, t);
               mx4_in_order();
@@ -379,7 +412,7 @@ __global__ __launch_bounds__(256, 2) void k_mx4_sweep(Mx4Rows x, int blocks, con
           b = fmaxf(b, ob);
         }
         const int64_t row = row0 + 16 * (wave * kF + f) + l16;
-        if (q == 0 && row < n) records[(int64_t)blockIdx.y * n + row] = Mx4Record{b, s, id};
+        if (q == 0 && row < n) records[(blockIdx.x - mx4_first_piece(cut, block)) * n + row] = Mx4Record{b, s, id};
       }
     }
   }
@@ -387,21 +420,28 @@ __global__ __launch_bounds__(256, 2) void k_mx4_sweep(Mx4Rows x, int blocks, con
 
 // ---------------------------------------------------------------- rows of any length
 // kCollect: the instances are those of list (counts->listed of them); the groups whose maximum reaches an instance's threshold are appended to its
-// list.  Otherwise one record per instance, share of the nodes (blockIdx.y) and half of the wavefronts.
+// list.  Otherwise one record per instance, piece of its block (Mx4Cut; a stage is a tile) and half of the wavefronts.
 template <bool kCollect>
 __global__ __launch_bounds__(512) void k_mx4_search(Mx4Operand x, Mx4Operand w, const float *__restrict__ init, int blocks,
-                                                    const void *__restrict__ zero16, int64_t tiles, Mx4Record *__restrict__ records,
+                                                    const void *__restrict__ zero16, Mx4Cut cut, Mx4Record *__restrict__ records,
                                                     const Mx4Counts *__restrict__ counts, const int *__restrict__ list,
                                                     const float *__restrict__ threshold, int *__restrict__ found,
                                                     int *__restrict__ groups) {
   typedef Mx4Sweep Tile;
   __shared__ __attribute__((aligned(16))) char smem[Tile::kLds];
-  const int64_t n = kCollect ? counts->listed : x.rows.n;
-  const int64_t per = (tiles + gridDim.y - 1) / gridDim.y, first = blockIdx.y * per, last = first + per < tiles ? first + per : tiles;
-  if (first >= last) return;
+  const int64_t n = kCollect ? counts->listed : x.rows.n, nb = (n + Tile::kRowsB - 1) / Tile::kRowsB;
+  if (kCollect) {
+    if (n == 0) return;
+    cut.per = (nb * cut.stages + gridDim.x - 1) / gridDim.x;
+  }
   const int64_t total = x.rows.n;
   x.rows.n = n;
-  for (int64_t row0 = (int64_t)blockIdx.x * Tile::kRowsB; row0 < n; row0 += (int64_t)gridDim.x * Tile::kRowsB) {
+  int64_t pos = blockIdx.x * cut.per;
+  const int64_t end = pos + cut.per < nb * cut.stages ? pos + cut.per : nb * cut.stages;
+  while (pos < end) {
+    const int64_t block = pos / cut.stages, row0 = block * Tile::kRowsB, first = pos - block * cut.stages;
+    const int64_t last = first + (end - pos) < cut.stages ? first + (end - pos) : cut.stages;
+    pos += last - first;
     Tile t;
     t.setup(smem, w, x, init, blocks, zero16);
     t.tile_b(row0, n, kCollect ? list : nullptr);
@@ -458,7 +498,7 @@ __global__ __launch_bounds__(512) void k_mx4_search(Mx4Operand x, Mx4Operand w, 
           b = fmaxf(b, ob);
         }
         const int64_t row = row0 + 16 * (t.wb * Tile::kFragB + v) + t.l16;
-        if (t.q == 0 && row < n) records[((int64_t)blockIdx.y * Tile::kWavesA + t.wa) * total + row] = Mx4Record{b, s, id};
+        if (t.q == 0 && row < n) records[((blockIdx.x - mx4_first_piece(cut, block)) * Tile::kWavesA + t.wa) * total + row] = Mx4Record{b, s, id};
       }
     }
   }
@@ -473,105 +513,135 @@ __device__ __forceinline__ double mx4_margin(double x2, float wmax2, int blocks)
   return 2.0 * (((blocks + 3) / 4 + 1) * kMx4Delta * size + 1e-34 * blocks);
 }
 
-// 16 instances a wavefront, lane l: instance l % 16; kMx4Batch of them at a time have the nodes of their groups fetched.  Bound by those loads (16 rows of
-// 64 bytes for one instruction, from L2).
-constexpr int kMx4Batch = 4;
-__global__ __launch_bounds__(256) void k_mx4_resolve(Mx4Rows x, Mx4Rows w, const float *__restrict__ init, int blocks,
-                                                     const Mx4Record *__restrict__ records, int shares, const float *__restrict__ parts,
+// `turns` (1, 2 or 4) times 16 instances a wavefront: lane l has instance l % (16 turns) of them for what an instance needs once - its records, its
+// margin, what becomes of it - and instance l % 16 of a turn for the products, for which the groups of kMx4Batch instances are fetched
+// together (1 KB a step in one piece of the stream).  A workgroup's instances that are left over take their places in the lists with one
+// addition: with one for every instance the additions, all to one word, would take as long as the rest.
+constexpr int kMx4Batch = 8;
+__global__ __launch_bounds__(256) void k_mx4_resolve(Mx4Rows x, const char *__restrict__ stream, int blocks, int turns,
+                                                     const Mx4Record *__restrict__ records, Mx4Cut cut, int halves, const float *__restrict__ parts,
                                                      int nparts, Mx4Counts *__restrict__ counts, int *__restrict__ list,
                                                      float *__restrict__ threshold, int *__restrict__ found, int *__restrict__ groups,
                                                      int32_t *__restrict__ bmus) {
   __shared__ float s_max[4];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q = lane >> 4;
+  __shared__ int s_count[2], s_base[2];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q = lane >> 4, steps = (blocks + 3) / 4;
+  const int64_t unit = mx4_stream_bytes(steps);
   float wmax2 = (int)threadIdx.x < nparts ? parts[threadIdx.x] : 0.f;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) wmax2 = fmaxf(wmax2, __shfl_xor(wmax2, o));
   if (lane == 0) s_max[wave] = wmax2;
+  if (threadIdx.x < 2) s_count[threadIdx.x] = 0;
   __syncthreads();
   wmax2 = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
-  const int64_t row0 = ((int64_t)blockIdx.x * 4 + wave) * 16, row = row0 + l16;
-  if (row0 >= x.n) return;
-  const int64_t xr = row < x.n ? row : x.n - 1;
-  float best = kMx4Lowest, second = kMx4Lowest;
-  int group = 0;
-  for (int s = 0; s < shares; ++s) {
-    const Mx4Record r = records[s * x.n + xr];
-    second = fmaxf(fmaxf(second, r.second), fminf(best, r.best));
-    group = r.best > best ? r.group : group;
-    best = fmaxf(best, r.best);
-  }
-  const i32x4 none = {0, 0, 0, 0};
-  mx_f32x4 mine = {0.f, 0.f, 0.f, 0.f};       // scores of nodes 16 group + 4 q ..
-  double x2 = 0.0;
-  bool nan = false;
+  const int64_t row0 = ((int64_t)blockIdx.x * 4 + wave) * 16 * turns, row = row0 + (lane & (16 * turns - 1));
+  int what = 0, where = -1, place = 0;           // which list the lane's instance goes to, its place of this workgroup's; the group, -1: all nodes
+  float reach = 0.f;
+  if (row0 < x.n) {
+    const int64_t xr = row < x.n ? row : x.n - 1;
+    float best = kMx4Lowest, second = kMx4Lowest;
+    int group = 0;
+    const int64_t block = xr / cut.rows, pieces = mx4_last_piece(cut, block) - mx4_first_piece(cut, block) + 1;
+    for (int64_t p = 0; p < pieces * halves; ++p) {
+      const Mx4Record r = records[p * x.n + xr];
+      second = fmaxf(fmaxf(second, r.second), fminf(best, r.best));
+      group = r.best > best ? r.group : group;
+      best = fmaxf(best, r.best);
+    }
+    double x2 = 0.0;                             // sum of the squares of the scales, NaN if one is
+    for (int turn = 0; turn < turns; ++turn) {
+      const int64_t tr = row0 + 16 * turn + l16 < x.n ? row0 + 16 * turn + l16 : x.n - 1;
+      double sum = 0.0;
+      for (int b0 = q; b0 < blocks; b0 += 16) {
+        int e[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) e[u] = x.scales[tr * blocks + (b0 + 4 * u < blocks ? b0 + 4 * u : blocks - 1)];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (b0 + 4 * u < blocks) sum += e[u] == 255 ? (double)NAN : mx4_pow2(2 * e[u] - 254);
+      }
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      if ((q & (turns - 1)) == turn) x2 = sum;
+    }
+    const bool nan = x2 != x2;
+    const double margin = mx4_margin(x2, wmax2, blocks);
+    reach = __double2float_rd((double)best - margin);
+    int near = 0, first = 0;
 #pragma unroll 1
-  for (int r0 = 0; r0 < 16; r0 += kMx4Batch) {
-    mx_f32x4 acc[kMx4Batch];
-    const uint8_t *wc[kMx4Batch], *ws[kMx4Batch];
+    for (int turn = 0; turn < turns; ++turn) {
+      if (row0 + 16 * turn >= x.n) break;
+      const int64_t tr = row0 + 16 * turn + l16 < x.n ? row0 + 16 * turn + l16 : x.n - 1;
+      mx_f32x4 mine = {0.f, 0.f, 0.f, 0.f};      // scores of nodes 4 q .. of instance l16's group
+#pragma unroll 1
+      for (int r0 = 0; r0 < 16; r0 += kMx4Batch) {
+        mx_f32x4 acc[kMx4Batch];
+        const char *base[kMx4Batch];
+        int part[kMx4Batch];
 #pragma unroll
-    for (int r = 0; r < kMx4Batch; ++r) {
-      const int64_t first = 16 * (int64_t)__shfl(group, r0 + r);
-      acc[r] = *reinterpret_cast<const mx_f32x4 *>(init + first + 4 * q);
-      const int64_t node = first + l16 < w.n ? first + l16 : w.n - 1;
-      wc[r] = w.codes + (node * blocks + q) * 16;
-      ws[r] = w.scales + node * blocks + q;
-    }
-    for (int b0 = 0; b0 < blocks; b0 += 4) {
-      const bool in = b0 + q < blocks;
-      const i32x4 xc = in ? *reinterpret_cast<const i32x4 *>(x.codes + (xr * blocks + b0 + q) * 16) : none;
-      const int xs = in ? x.scales[xr * blocks + b0 + q] : 0;
-      if (r0 == 0 && in) {
-        x2 += mx4_pow2(2 * xs - 254);
-        nan |= xs == 255;
+        for (int r = 0; r < kMx4Batch; ++r) {
+          const int g = __builtin_amdgcn_readlane(group, 16 * turn + r0 + r);
+          base[r] = stream + (g >> 2) * unit;
+          part[r] = g & 3;
+          acc[r] = *reinterpret_cast<const mx_f32x4 *>(base[r] + steps * 4352 + part[r] * 64 + q * 16);
+        }
+        for (int s = 0; s < steps; ++s) {
+          i32x4 c[kMx4Batch];
+          int e[kMx4Batch];
+#pragma unroll
+          for (int r = 0; r < kMx4Batch; ++r) {
+            c[r] = *reinterpret_cast<const i32x4 *>(base[r] + s * 4096 + part[r] * 1024 + lane * 16);
+            e[r] = *reinterpret_cast<const int *>(base[r] + steps * 4096 + s * 256 + part[r] * 16 + q * 64 + (l16 & 3) * 4);
+          }
+          const int64_t b = tr * blocks + (4 * s + q < blocks ? 4 * s + q : blocks - 1);
+          const i32x4 xc = *reinterpret_cast<const i32x4 *>(x.codes + b * 16);
+          const int xs = x.scales[b];
+#pragma unroll
+          for (int r = 0; r < kMx4Batch; ++r) acc[r] = mx4_mfma<0, 0>(c[r], xc, acc[r], e[r] >> (8 * (l16 >> 2)), xs);
+        }
+#pragma unroll
+        for (int r = 0; r < kMx4Batch; ++r)
+          if (l16 == r0 + r) mine = acc[r];
       }
-      i32x4 c[kMx4Batch];
-      int e[kMx4Batch];
+      const float limit = __shfl(reach, 16 * turn + l16);
+      int hits = 0, lowest = 16;
 #pragma unroll
-      for (int r = 0; r < kMx4Batch; ++r) {
-        c[r] = in ? *reinterpret_cast<const i32x4 *>(wc[r] + b0 * 16) : none;
-        e[r] = in ? ws[r][b0] : 0;
+      for (int u = 3; u >= 0; --u)
+        if (mine[u] >= limit) { ++hits; lowest = 4 * q + u; }
+#pragma unroll
+      for (int o = 16; o < 64; o <<= 1) {
+        hits += __shfl_xor(hits, o);
+        lowest = min(lowest, __shfl_xor(lowest, o));
       }
-#pragma unroll
-      for (int r = 0; r < kMx4Batch; ++r) acc[r] = mx4_mfma<0, 0>(c[r], xc, acc[r], e[r], xs);
+      if ((q & (turns - 1)) == turn) { near = hits; first = lowest; }
     }
-#pragma unroll
-    for (int r = 0; r < kMx4Batch; ++r)
-      if (l16 == r0 + r) mine = acc[r];
+    if (lane < 16 * turns && row < x.n) {
+      if (nan) {                                 // no finite distance to any node
+        bmus[row] = 0;
+      } else if (!(margin < INFINITY) || !(best > kMx4Lowest)) {
+        where = 1;
+        what = -1;
+      } else if (second >= reach) {
+        where = 0;
+      } else if (near == 1) {
+        bmus[row] = 16 * group + first;
+      } else {
+        where = 1;
+        what = group;
+      }
+      if (where >= 0) place = atomicAdd(&s_count[where], 1);
+    }
   }
-  x2 += __shfl_xor(x2, 16);
-  x2 += __shfl_xor(x2, 32);
-  nan |= __shfl_xor((int)nan, 16) != 0;
-  nan |= __shfl_xor((int)nan, 32) != 0;
-  const double margin = mx4_margin(x2, wmax2, blocks);
-  const float reach = __double2float_rd((double)best - margin);
-  int near = 0, first = 0x7fffffff;
-#pragma unroll
-  for (int u = 3; u >= 0; --u)
-    if (mine[u] >= reach) { ++near; first = 16 * group + 4 * q + u; }
-#pragma unroll
-  for (int o = 16; o < 64; o <<= 1) {
-    near += __shfl_xor(near, o);
-    first = min(first, __shfl_xor(first, o));
-  }
-  if (q != 0 || row >= x.n) return;
-  if (nan) {                                   // no finite distance to any node
-    bmus[row] = 0;
-  } else if (!(margin < INFINITY) || !(best > kMx4Lowest)) {
-    const int64_t slot = x.n - 1 - atomicAdd(&counts->single, 1);
-    list[slot] = (int)row;
-    found[slot] = kMx4List + 1;
-  } else if (second >= reach) {
-    const int slot = atomicAdd(&counts->listed, 1);
+  __syncthreads();
+  if (threadIdx.x < 2 && s_count[threadIdx.x] > 0)
+    s_base[threadIdx.x] = atomicAdd(threadIdx.x == 0 ? &counts->listed : &counts->single, s_count[threadIdx.x]);
+  __syncthreads();
+  if (where >= 0) {
+    const int64_t slot = where == 0 ? s_base[0] + place : x.n - 1 - (s_base[1] + place);
     list[slot] = (int)row;
     threshold[slot] = reach;
-    found[slot] = 0;
-  } else if (near == 1) {
-    bmus[row] = first;
-  } else {
-    const int64_t slot = x.n - 1 - atomicAdd(&counts->single, 1);
-    list[slot] = (int)row;
-    found[slot] = 1;
-    groups[slot * kMx4List] = group;
+    found[slot] = where == 0 ? 0 : what < 0 ? kMx4List + 1 : 1;
+    if (where == 1 && what >= 0) groups[slot * kMx4List] = what;
   }
 }
 
@@ -591,13 +661,25 @@ __global__ __launch_bounds__(256) void k_mx4_exact(Mx4Rows x, Mx4Rows w, int blo
     for (int64_t g = 0; g < ng; ++g) {
       const int64_t node = 16 * (all ? g : (int64_t)groups[slot * kMx4List + g]) + l16, wr = node < w.n ? node : w.n - 1;
       double s = 0.0;
-      for (int b = q; b < blocks; b += 4) {
-        const int ex = x.scales[row * blocks + b], ew = w.scales[wr * blocks + b];
-        float xw, ww;
-        mx4_block_dots(*reinterpret_cast<const i32x4 *>(x.codes + (row * blocks + b) * 16),
-                       *reinterpret_cast<const i32x4 *>(w.codes + (wr * blocks + b) * 16), xw, ww);
-        s += (double)xw * mx4_pow2(ex + ew - 254) - (double)ww * mx4_pow2(2 * ew - 255);
-        if (ex == 255 || ew == 255) s = NAN;
+      for (int b0 = q; b0 < blocks; b0 += 16) {
+        i32x4 xc[4], wc[4];
+        int ex[4], ew[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int b = b0 + 4 * u < blocks ? b0 + 4 * u : blocks - 1;      // (a load under a condition would be waited for by itself)
+          xc[u] = *reinterpret_cast<const i32x4 *>(x.codes + (row * blocks + b) * 16);
+          wc[u] = *reinterpret_cast<const i32x4 *>(w.codes + (wr * blocks + b) * 16);
+          ex[u] = x.scales[row * blocks + b];
+          ew[u] = w.scales[wr * blocks + b];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          float xw, ww;
+          mx4_block_dots(xc[u], wc[u], xw, ww);
+          double part = (double)xw * mx4_pow2(ex[u] + ew[u] - 254) - (double)ww * mx4_pow2(2 * ew[u] - 255);
+          if (ex[u] == 255 || ew[u] == 255) part = NAN;
+          s += b0 + 4 * u < blocks ? part : 0.0;
+        }
       }
       s += __shfl_xor(s, 16);
       s += __shfl_xor(s, 32);
@@ -613,51 +695,43 @@ __global__ __launch_bounds__(256) void k_mx4_exact(Mx4Rows x, Mx4Rows w, int blo
   }
 }
 
-// How the matrix cores' passes are laid out: instances a workgroup takes, stages or tiles of nodes, shares of those, records of an instance.
+// How the pass over all instances is laid out.
 struct Mx4Layout {
   bool sweep;              // k_mx4_sweep, else k_mx4_search
-  int rows, shares, records;
-  int64_t stages, padded;  // padded: nodes rounded up to whole stages
+  Mx4Cut cut;
+  int grid, records;       // workgroups; records of an instance
+  int64_t padded;          // nodes rounded up to whole stages
 };
 
 template <int kT>
-static void sweep_shape(int steps, int *rows, int *nodes, int *cost) {
+static void sweep_shape(int steps, int *rows, int *nodes) {
   if (steps == kT) {
-    typedef typename Mx4ShapeOf<kT>::type Shape;
+    typedef typename Mx4ShapeOf<kT, false>::type Shape;
     *rows = Shape::rows;
     *nodes = 64 * Shape::units;
-    *cost = Shape::units * Shape::F * kT;
   }
 }
 
-// The shares are those with the fewest rounds of workgroups times what one takes: its stages, and its instances' loads.
 static Mx4Layout search_layout(const som_ctx *c, int64_t n) {
   Mx4Layout l;
   const int steps = (mx4_blocks(c->dim) + 3) / 4;
-  int nodes = Mx4Sweep::kRowsA, cost = 0;
+  int nodes = Mx4Sweep::kRowsA;
   l.sweep = steps <= kMx4SweepSteps;
-  l.rows = Mx4Sweep::kRowsB;
+  l.cut.rows = Mx4Sweep::kRowsB;
   if (l.sweep) {
-    sweep_shape<1>(steps, &l.rows, &nodes, &cost); sweep_shape<2>(steps, &l.rows, &nodes, &cost);
-    sweep_shape<3>(steps, &l.rows, &nodes, &cost); sweep_shape<4>(steps, &l.rows, &nodes, &cost);
-    sweep_shape<5>(steps, &l.rows, &nodes, &cost); sweep_shape<6>(steps, &l.rows, &nodes, &cost);
-    sweep_shape<7>(steps, &l.rows, &nodes, &cost); sweep_shape<8>(steps, &l.rows, &nodes, &cost);
-  } else {
-    cost = 32 * steps;
+    sweep_shape<1>(steps, &l.cut.rows, &nodes); sweep_shape<2>(steps, &l.cut.rows, &nodes);
+    sweep_shape<3>(steps, &l.cut.rows, &nodes); sweep_shape<4>(steps, &l.cut.rows, &nodes);
+    sweep_shape<5>(steps, &l.cut.rows, &nodes); sweep_shape<6>(steps, &l.cut.rows, &nodes);
+    sweep_shape<7>(steps, &l.cut.rows, &nodes); sweep_shape<8>(steps, &l.cut.rows, &nodes);
   }
-  l.stages = ((int64_t)c->k + nodes - 1) / nodes;
-  l.padded = l.stages * nodes;
-  const int64_t nb = (n + l.rows - 1) / l.rows, at_once = (l.sweep ? 2 : 1) * (int64_t)c->n_cu;
-  int64_t least = 0;
-  l.shares = 1;
-  for (int s = 1; s <= l.stages && s <= 64; ++s) {
-    const int64_t rounds = (nb * s + at_once - 1) / at_once, total = rounds * ((l.stages + s - 1) / s * cost + 64);
-    if (s == 1 || total < least) {
-      least = total;
-      l.shares = s;
-    }
-  }
-  l.records = l.shares * (l.sweep ? 1 : Mx4Sweep::kWavesA);
+  l.cut.stages = ((int64_t)c->k + nodes - 1) / nodes;
+  l.padded = l.cut.stages * nodes;
+  const int64_t all = (n + l.cut.rows - 1) / l.cut.rows * l.cut.stages, most = (l.sweep ? 2 : 1) * (int64_t)c->n_cu;
+  l.cut.per = (all + most - 1) / most;
+  l.grid = (int)((all + l.cut.per - 1) / l.cut.per);
+  // pieces that a block's stages can be spread over
+  const int64_t pieces = (l.cut.stages + l.cut.per - 2) / l.cut.per + 1;
+  l.records = (int)(pieces < l.grid ? pieces : l.grid) * (l.sweep ? 1 : Mx4Sweep::kWavesA);
   return l;
 }
 
@@ -685,10 +759,10 @@ static Mx4SearchScratch search_scratch(const som_ctx *c, int64_t n, const Mx4Lay
     at += (bytes + 255) / 256 * 256;
     return p;
   };
-  m.init = static_cast<float *>(take((size_t)l.padded * 4));
+  m.init = static_cast<float *>(take(l.sweep ? 0 : (size_t)l.padded * 4));
   m.parts = static_cast<float *>(take(kMx4NodeBlocks * 4));
   m.counts = static_cast<Mx4Counts *>(take(sizeof(Mx4Counts)));
-  m.stream = static_cast<char *>(take(l.sweep ? (size_t)(l.padded / 64) * mx4_stream_bytes(steps) : 0));
+  m.stream = static_cast<char *>(take((size_t)(l.padded / 64) * mx4_stream_bytes(steps)));
   m.packed_w = static_cast<int *>(take(l.sweep ? 0 : mx4_packed_bytes(c->k, blocks)));
   m.packed_x = static_cast<int *>(take(l.sweep ? 0 : mx4_packed_bytes(n, blocks)));
   m.records = static_cast<Mx4Record *>(take((size_t)l.records * N * sizeof(Mx4Record)));
@@ -708,7 +782,7 @@ size_t mx4_search_bytes(const som_ctx *c, int64_t n) {
 
 template <int kT, bool kCollect>
 static void launch_sweep(som_ctx *c, Mx4Rows x, const Mx4Layout &l, const Mx4SearchScratch &m, dim3 grid) {
-  hipLaunchKernelGGL((k_mx4_sweep<kT, kCollect>), grid, dim3(256), 0, c->stream, x, mx4_blocks(c->dim), m.stream, l.padded / 64, m.records,
+  hipLaunchKernelGGL((k_mx4_sweep<kT, kCollect>), grid, dim3(256), 0, c->stream, x, mx4_blocks(c->dim), m.stream, l.cut, m.records,
                      m.counts, m.list, m.threshold, m.found, m.groups);
 }
 
@@ -716,12 +790,7 @@ static void launch_sweep(som_ctx *c, Mx4Rows x, const Mx4Layout &l, const Mx4Sea
 template <bool kCollect>
 static hipError_t launch_pass(som_ctx *c, Mx4Rows x, Mx4Rows w, const Mx4Layout &l, const Mx4SearchScratch &m) {
   const int blocks = mx4_blocks(c->dim);
-  const int64_t nb = (x.n + l.rows - 1) / l.rows;
-  dim3 grid((unsigned)nb, l.shares);
-  if (kCollect) {
-    const unsigned ways = (unsigned)(l.stages < 16 ? l.stages : 16), most = 2 * c->n_cu / ways;
-    grid = dim3((unsigned)(nb < most ? nb : most), ways);
-  }
+  const dim3 grid(kCollect ? (l.sweep ? 2 : 1) * c->n_cu : l.grid);
   if (l.sweep) {
     switch ((blocks + 3) / 4) {
       case 1: launch_sweep<1, kCollect>(c, x, l, m, grid); break;
@@ -739,7 +808,7 @@ static hipError_t launch_pass(som_ctx *c, Mx4Rows x, Mx4Rows w, const Mx4Layout 
                                               kCollect ? &m.counts->listed : nullptr);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(k_mx4_search<kCollect>, grid, dim3(Mx4Sweep::kThreads), 0, c->stream, Mx4Operand{x, m.packed_x}, Mx4Operand{w, m.packed_w},
-                     m.init, blocks, c->zero16, l.stages, m.records, m.counts, m.list, m.threshold, m.found, m.groups);
+                     m.init, blocks, c->zero16, l.cut, m.records, m.counts, m.list, m.threshold, m.found, m.groups);
   return hipGetLastError();
 }
 
@@ -749,12 +818,15 @@ hipError_t launch_bmu_mx4(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int32
   const Mx4SearchScratch m = search_scratch(c, x.n, l, scratch);
   const int blocks = mx4_blocks(c->dim);
   const int parts = l.padded / 64 < kMx4NodeBlocks ? (int)(l.padded / 64) : kMx4NodeBlocks;
-  if (l.sweep) hipLaunchKernelGGL(k_mx4_nodes<true>, dim3(parts), dim3(256), 0, c->stream, w, blocks, l.padded, m.init, m.stream, m.packed_w, m.parts, m.counts);
-  else hipLaunchKernelGGL(k_mx4_nodes<false>, dim3(parts), dim3(256), 0, c->stream, w, blocks, l.padded, m.init, m.stream, m.packed_w, m.parts, m.counts);
+  hipLaunchKernelGGL(k_mx4_nodes, dim3(parts), dim3(256), 0, c->stream, w, blocks, l.padded, l.sweep ? nullptr : m.init, m.stream,
+                     l.sweep ? nullptr : m.packed_w, m.parts, m.counts);
   hipError_t e = launch_pass<false>(c, x, w, l, m);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k_mx4_resolve, dim3((unsigned)((x.n + 63) / 64)), dim3(256), 0, c->stream, x, w, m.init, blocks, m.records, l.records,
-                     m.parts, parts, m.counts, m.list, m.threshold, m.found, m.groups, bmus);
+  // (fewer turns where there are not enough instances for as many workgroups as the chip holds)
+  const int64_t by64 = (x.n + 63) / 64;
+  const int turns = by64 >= 32 * (int64_t)c->n_cu ? 4 : by64 >= 16 * (int64_t)c->n_cu ? 2 : 1;
+  hipLaunchKernelGGL(k_mx4_resolve, dim3((unsigned)((by64 + turns - 1) / turns)), dim3(256), 0, c->stream, x, m.stream, blocks, turns,
+                     m.records, l.cut, l.sweep ? 1 : Mx4Sweep::kWavesA, m.parts, parts, m.counts, m.list, m.threshold, m.found, m.groups, bmus);
   e = launch_pass<true>(c, x, w, l, m);
   if (e != hipSuccess) return e;
   const int64_t most = (x.n + 3) / 4;

@@ -50,19 +50,19 @@ __global__ __launch_bounds__(256) void k_mx4_product_few(Mx4Rows a, Mx4Rows b, i
     if (jb[t] >= b.n) jb[t] = b.n - 1;
   }
   mx_f32x4 acc[4] = {};
-  const i32x4 none = {0, 0, 0, 0};
   for (int k0 = 0; k0 < blocks; k0 += 4) {
-    const int k = k0 + q;
-    const bool in = k < blocks;
-    const i32x4 x = in ? *reinterpret_cast<const i32x4 *>(a.codes + (ia * blocks + k) * 16) : none;
-    const int sx = in ? a.scales[ia * blocks + k] : 0;
+    const bool in = k0 + q < blocks;
+    const int k = in ? k0 + q : blocks - 1;      // (a load under a condition would be waited for by itself)
+    i32x4 x = *reinterpret_cast<const i32x4 *>(a.codes + (ia * blocks + k) * 16);
+    const int sx = a.scales[ia * blocks + k];
     i32x4 y[4];
     int sy[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      y[t] = in ? *reinterpret_cast<const i32x4 *>(b.codes + (jb[t] * blocks + k) * 16) : none;
-      sy[t] = in ? b.scales[jb[t] * blocks + k] : 0;
+      y[t] = *reinterpret_cast<const i32x4 *>(b.codes + (jb[t] * blocks + k) * 16);
+      sy[t] = b.scales[jb[t] * blocks + k];
     }
+    if (!in) x = i32x4{0, 0, 0, 0};
 #pragma unroll
     for (int t = 0; t < 4; ++t) acc[t] = mx4_mfma<0, 0>(y[t], x, acc[t], sy[t], sx);
   }

@@ -204,6 +204,15 @@ def test_search_among_copies(n, k, dim):
     check_search(R.quantize(rng.standard_normal((n, dim))), w, dim)
 
 
+@pytest.mark.parametrize("dim", [100, 200, 300, 500, 600, 700, 800, 1000, 1100, 2100])
+def test_search_among_twins(dim):
+    """Every node twice, far apart: two groups are equally near for every instance, and the first of the two nodes is right."""
+    rng = np.random.default_rng(dim)
+    n, k = 2000, 2600
+    half = rng.standard_normal((k // 2, dim))
+    check_search(R.quantize(rng.standard_normal((n, dim))), R.quantize(np.concatenate([half, half[rng.permutation(k // 2)]])), dim)
+
+
 @pytest.mark.parametrize("n,k,dim", [(2, 100, 64), (2000, 1000, 64), (300, 300, 1200), (5000, 3000, 64), (1000, 500, 1200)])
 def test_search_on_a_coarse_grid(n, k, dim):
     """Small whole numbers: many nodes are equally near."""
