@@ -210,21 +210,21 @@ __global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int64_
 // The compiler keeps reads, products and maxima apart unless the order is fixed, as it is here.  Two stages in LDS of kUnits times 64 nodes: a
 // piece is read into registers while the one before it is multiplied, so when the last of a stage begins the stage is free and gets the
 // loads of the one after the next.
-template <int kT, int kF, int kUnits>
+template <int kT, int kF, int kUnits, int kWavesPerSimd>
 struct Mx4SweepShape {
-  static constexpr int F = kF, units = kUnits, rows = 64 * kF;
+  static constexpr int F = kF, units = kUnits, rows = 64 * kF, waves = kWavesPerSimd;
   static constexpr int unit = mx4_stream_bytes(kT), stage = kUnits * unit, rest = unit / 1024 - 4 * kT, lds = 2 * stage;
 };
-// F: as many as two wavefronts a SIMD leave registers for (one fewer with the lists to write).
-template <int kT, bool kCollect> struct Mx4ShapeOf;
-template <bool kCollect> struct Mx4ShapeOf<1, kCollect> { typedef Mx4SweepShape<1, 8, 4> type; };
-template <bool kCollect> struct Mx4ShapeOf<2, kCollect> { typedef Mx4SweepShape<2, kCollect ? 5 : 6, 2> type; };
-template <bool kCollect> struct Mx4ShapeOf<3, kCollect> { typedef Mx4SweepShape<3, kCollect ? 4 : 5, 2> type; };
-template <bool kCollect> struct Mx4ShapeOf<4, kCollect> { typedef Mx4SweepShape<4, kCollect ? 3 : 4, 1> type; };
-template <bool kCollect> struct Mx4ShapeOf<5, kCollect> { typedef Mx4SweepShape<5, kCollect ? 3 : 4, 1> type; };
-template <bool kCollect> struct Mx4ShapeOf<6, kCollect> { typedef Mx4SweepShape<6, kCollect ? 2 : 4, 1> type; };
-template <bool kCollect> struct Mx4ShapeOf<7, kCollect> { typedef Mx4SweepShape<7, kCollect ? 2 : 3, 1> type; };
-template <bool kCollect> struct Mx4ShapeOf<8, kCollect> { typedef Mx4SweepShape<8, kCollect ? 2 : 3, 1> type; };
+// F: as many as two wavefronts a SIMD leave registers for (one fewer with the lists to write); from 7 steps on a single wavefront with twice
+// as many (100,000 x 10,000, whole search, us, two wavefronts / one: 384 features 201 / 222, 512 262 / 284, 640 320 / 335, 768 383 / 409,
+// 900 542 / 528, 1,000 597 / 589).
+template <int kT, bool kCollect> struct Mx4ShapeOf { typedef Mx4SweepShape<kT, kCollect ? 3 : 4, 1, 2> type; };
+template <bool kCollect> struct Mx4ShapeOf<1, kCollect> { typedef Mx4SweepShape<1, 8, 4, 2> type; };
+template <bool kCollect> struct Mx4ShapeOf<2, kCollect> { typedef Mx4SweepShape<2, kCollect ? 5 : 6, 2, 2> type; };
+template <bool kCollect> struct Mx4ShapeOf<3, kCollect> { typedef Mx4SweepShape<3, kCollect ? 4 : 5, 2, 2> type; };
+template <bool kCollect> struct Mx4ShapeOf<6, kCollect> { typedef Mx4SweepShape<6, kCollect ? 2 : 4, 1, 2> type; };
+template <bool kCollect> struct Mx4ShapeOf<7, kCollect> { typedef Mx4SweepShape<7, kCollect ? 4 : 6, 1, 1> type; };
+template <bool kCollect> struct Mx4ShapeOf<8, kCollect> { typedef Mx4SweepShape<8, kCollect ? 4 : 6, 1, 1> type; };
 constexpr int kMx4SweepSteps = 8;
 
 // The work of a pass, (block of instances, stage of nodes) pairs in that order, is cut into one piece of `per` stages for every workgroup, so
@@ -245,7 +245,7 @@ __device__ __forceinline__ void mx4_in_order() {
 
 // kCollect as in k_mx4_search.
 template <int kT, bool kCollect>
-__global__ __launch_bounds__(256, 2) void k_mx4_sweep(Mx4Rows x, int blocks, const char *__restrict__ stream, Mx4Cut cut,
+__global__ __launch_bounds__(256, (Mx4ShapeOf<kT, kCollect>::type::waves)) void k_mx4_sweep(Mx4Rows x, int blocks, const char *__restrict__ stream, Mx4Cut cut,
                                                       Mx4Record *__restrict__ records, const Mx4Counts *__restrict__ counts,
                                                       const int *__restrict__ list, const float *__restrict__ threshold,
                                                       int *__restrict__ found, int *__restrict__ groups) {
@@ -645,7 +645,8 @@ __global__ __launch_bounds__(256) void k_mx4_resolve(Mx4Rows x, const char *__re
   }
 }
 
-// A wavefront an instance: lane l has node l % 16 of a group and every fourth block.
+// A wavefront an instance: lane l has node l % 16 of a group and every fourth block, kEach of those at a time.
+template <int kEach>
 __global__ __launch_bounds__(256) void k_mx4_exact(Mx4Rows x, Mx4Rows w, int blocks, const Mx4Counts *__restrict__ counts,
                                                    const int *__restrict__ list, const int *__restrict__ found,
                                                    const int *__restrict__ groups, int32_t *__restrict__ bmus) {
@@ -661,11 +662,11 @@ __global__ __launch_bounds__(256) void k_mx4_exact(Mx4Rows x, Mx4Rows w, int blo
     for (int64_t g = 0; g < ng; ++g) {
       const int64_t node = 16 * (all ? g : (int64_t)groups[slot * kMx4List + g]) + l16, wr = node < w.n ? node : w.n - 1;
       double s = 0.0;
-      for (int b0 = q; b0 < blocks; b0 += 16) {
-        i32x4 xc[4], wc[4];
-        int ex[4], ew[4];
+      for (int b0 = q; b0 < blocks; b0 += 4 * kEach) {
+        i32x4 xc[kEach], wc[kEach];
+        int ex[kEach], ew[kEach];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < kEach; ++u) {
           const int b = b0 + 4 * u < blocks ? b0 + 4 * u : blocks - 1;      // (a load under a condition would be waited for by itself)
           xc[u] = *reinterpret_cast<const i32x4 *>(x.codes + (row * blocks + b) * 16);
           wc[u] = *reinterpret_cast<const i32x4 *>(w.codes + (wr * blocks + b) * 16);
@@ -673,7 +674,7 @@ __global__ __launch_bounds__(256) void k_mx4_exact(Mx4Rows x, Mx4Rows w, int blo
           ew[u] = w.scales[wr * blocks + b];
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < kEach; ++u) {
           float xw, ww;
           mx4_block_dots(xc[u], wc[u], xw, ww);
           double part = (double)xw * mx4_pow2(ex[u] + ew[u] - 254) - (double)ww * mx4_pow2(2 * ew[u] - 255);
@@ -704,10 +705,11 @@ struct Mx4Layout {
 };
 
 template <int kT>
-static void sweep_shape(int steps, int *rows, int *nodes) {
+static void sweep_shape(int steps, int *rows, int *nodes, int *at_once) {
   if (steps == kT) {
     typedef typename Mx4ShapeOf<kT, false>::type Shape;
     *rows = Shape::rows;
+    *at_once = Shape::waves;
     *nodes = 64 * Shape::units;
   }
 }
@@ -715,18 +717,18 @@ static void sweep_shape(int steps, int *rows, int *nodes) {
 static Mx4Layout search_layout(const som_ctx *c, int64_t n) {
   Mx4Layout l;
   const int steps = (mx4_blocks(c->dim) + 3) / 4;
-  int nodes = Mx4Sweep::kRowsA;
+  int nodes = Mx4Sweep::kRowsA, at_once = 1;      // nodes of a stage, workgroups a CU holds
   l.sweep = steps <= kMx4SweepSteps;
   l.cut.rows = Mx4Sweep::kRowsB;
   if (l.sweep) {
-    sweep_shape<1>(steps, &l.cut.rows, &nodes); sweep_shape<2>(steps, &l.cut.rows, &nodes);
-    sweep_shape<3>(steps, &l.cut.rows, &nodes); sweep_shape<4>(steps, &l.cut.rows, &nodes);
-    sweep_shape<5>(steps, &l.cut.rows, &nodes); sweep_shape<6>(steps, &l.cut.rows, &nodes);
-    sweep_shape<7>(steps, &l.cut.rows, &nodes); sweep_shape<8>(steps, &l.cut.rows, &nodes);
+    sweep_shape<1>(steps, &l.cut.rows, &nodes, &at_once); sweep_shape<2>(steps, &l.cut.rows, &nodes, &at_once);
+    sweep_shape<3>(steps, &l.cut.rows, &nodes, &at_once); sweep_shape<4>(steps, &l.cut.rows, &nodes, &at_once);
+    sweep_shape<5>(steps, &l.cut.rows, &nodes, &at_once); sweep_shape<6>(steps, &l.cut.rows, &nodes, &at_once);
+    sweep_shape<7>(steps, &l.cut.rows, &nodes, &at_once); sweep_shape<8>(steps, &l.cut.rows, &nodes, &at_once);
   }
   l.cut.stages = ((int64_t)c->k + nodes - 1) / nodes;
   l.padded = l.cut.stages * nodes;
-  const int64_t all = (n + l.cut.rows - 1) / l.cut.rows * l.cut.stages, most = (l.sweep ? 2 : 1) * (int64_t)c->n_cu;
+  const int64_t all = (n + l.cut.rows - 1) / l.cut.rows * l.cut.stages, most = at_once * (int64_t)c->n_cu;
   l.cut.per = (all + most - 1) / most;
   l.grid = (int)((all + l.cut.per - 1) / l.cut.per);
   // pieces that a block's stages can be spread over
@@ -830,8 +832,9 @@ hipError_t launch_bmu_mx4(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int32
   e = launch_pass<true>(c, x, w, l, m);
   if (e != hipSuccess) return e;
   const int64_t most = (x.n + 3) / 4;
-  hipLaunchKernelGGL(k_mx4_exact, dim3((unsigned)(most < 8 * c->n_cu ? most : 8 * c->n_cu)), dim3(256), 0, c->stream, x, w, blocks, m.counts,
-                     m.list, m.found, m.groups, bmus);
+  const dim3 grid((unsigned)(most < 8 * c->n_cu ? most : 8 * c->n_cu));
+  if (blocks > 8) hipLaunchKernelGGL(k_mx4_exact<4>, grid, dim3(256), 0, c->stream, x, w, blocks, m.counts, m.list, m.found, m.groups, bmus);
+  else hipLaunchKernelGGL(k_mx4_exact<1>, grid, dim3(256), 0, c->stream, x, w, blocks, m.counts, m.list, m.found, m.groups, bmus);
   return hipGetLastError();
 }
 

@@ -77,43 +77,79 @@ __global__ __launch_bounds__(256) void k_mx4_product_few(Mx4Rows a, Mx4Rows b, i
 }
 
 // ---------------------------------------------------------------- tiles
-// kVec: rows of the output begin at 16-byte boundaries.
-template <typename T, typename Tile, bool kVec>
-__global__ __launch_bounds__(512) void k_mx4_product(Mx4Operand a, Mx4Operand b, int blocks, const void *__restrict__ zero16,
-                                                     T *__restrict__ out, int64_t stride, unsigned tiles_j) {
+// A wavefront's results leave through LDS, 16 rows at a time, so that its stores are whole stretches of a row (written as the lanes hold them, 32 or 64
+// bytes of 16 rows an instruction, 50,000 x 10,000 products of 256 features to bf16 took 392 us).  kWidth bytes a lane.
+template <typename T, int kCols, int kWidth>
+__device__ __forceinline__ void mx4_store_rows(const T *block, int pitch, T *__restrict__ out, int64_t stride, int64_t rows, int64_t cols, int lane) {
+  constexpr int kEach = kWidth / (int)sizeof(T), kLanes = kCols / kEach, kAtOnce = kLanes < 64 ? 64 / kLanes : 1;
+  typedef T Vec __attribute__((ext_vector_type(kEach)));
+#pragma unroll
+  for (int r0 = 0; r0 < 16; r0 += kAtOnce)
+#pragma unroll
+    for (int c0 = 0; c0 < kLanes; c0 += 64) {
+      const int r = r0 + (kLanes < 64 ? lane / kLanes : 0), c = (c0 + (kLanes < 64 ? lane % kLanes : lane)) * kEach;
+      if (r >= rows || c >= cols) continue;
+      const T *src = block + r * pitch + c;
+      T *dst = out + r * stride + c;
+      if (c + kEach <= cols) {
+        *reinterpret_cast<Vec *>(dst) = *reinterpret_cast<const Vec *>(src);
+      } else {
+#pragma unroll
+        for (int u = 0; u < kEach; ++u)
+          if (c + u < cols) dst[u] = src[u];
+      }
+    }
+}
+
+constexpr int kMx4Band = 8;
+
+// width: bytes that the rows of the output are aligned to, 16, 4 or 2.
+template <typename T, typename Tile, bool kStretch>
+__global__ __launch_bounds__(512, (Tile::kFragB == 2 ? 4 : 2)) void k_mx4_product(Mx4Operand a, Mx4Operand b, int blocks, const void *__restrict__ zero16,
+                                                     T *__restrict__ out, int64_t stride, unsigned tiles_j, int width) {
+  constexpr int kCols = 16 * Tile::kFragA, kPitch = kCols + 16 / (int)sizeof(T);
   __shared__ __attribute__((aligned(16))) char smem[Tile::kLds];
+  static_assert(Tile::kWaves * 16 * kPitch * (int)sizeof(T) <= Tile::kLds, "the results of 16 rows of every wavefront");
   Tile t;
-  const unsigned ti = blockIdx.x / tiles_j, tj = blockIdx.x - ti * tiles_j;
+  // Workgroups are dealt to the eight XCDs in turn.  Where the output is most of the work each XCD gets a stretch of consecutive tiles, kMx4Band
+  // rows of tiles column by column, so that the lines of the output that two tiles share meet in one L2 and so do the operands (to bf16, us, as
+  // dealt / stretches of rows of tiles / in bands: 50,000 x 10,000 x 256 371 / 321 / 254, 384 - / 378 / 308; but 8,192 x 8,192 x 4,096 163 / 174 / 172).
+  unsigned ti = blockIdx.x / tiles_j, tj = blockIdx.x - ti * tiles_j;
+  if (kStretch) {
+    const unsigned share = gridDim.x / 8, spare = gridDim.x % 8, x = blockIdx.x % 8;
+    const unsigned tile = x * share + (x < spare ? x : spare) + blockIdx.x / 8;
+    const unsigned band = tile / (kMx4Band * tiles_j), in_band = tile - band * kMx4Band * tiles_j;
+    const unsigned high = min((unsigned)kMx4Band, gridDim.x / tiles_j - band * kMx4Band);
+    tj = in_band / high;
+    ti = band * kMx4Band + in_band - tj * high;
+  }
   t.setup(smem, b, a, nullptr, blocks, zero16);
-  const int64_t i0 = (int64_t)ti * Tile::kRowsB, j0 = (int64_t)tj * Tile::kRowsA;
+  const int64_t i0 = (int64_t)ti * Tile::kRowsB, j0 = (int64_t)tj * Tile::kRowsA + t.wa * kCols;
   t.tile_b(i0, a.rows.n, nullptr);
   t.run(tj, tj + 1, [](int64_t) {});
-  const int64_t m = b.rows.n;
+  T *block = reinterpret_cast<T *>(smem) + t.wave * 16 * kPitch;
 #pragma unroll
   for (int v = 0; v < Tile::kFragB; ++v) {
-    const int64_t i = i0 + 16 * (t.wb * Tile::kFragB + v) + t.l16;
 #pragma unroll
     for (int g = 0; g < Tile::kFragA / 4; ++g) {
-      const int64_t j = j0 + 64 * (t.wa * (Tile::kFragA / 4) + g) + 16 * t.q;
       T row[16];
 #pragma unroll
       for (int u = 0; u < 16; ++u) row[u] = (T)t.acc[4 * g + u / 4][v][u & 3];
-      if (i < a.rows.n) {
-        T *dst = out + i * stride + j;
-        if (kVec && j + 16 <= m) {
 #pragma unroll
-          for (int u = 0; u < (int)sizeof(T); ++u) reinterpret_cast<i32x4 *>(dst)[u] = reinterpret_cast<const i32x4 *>(row)[u];
-        } else {
-#pragma unroll
-          for (int u = 0; u < 16; ++u)
-            if (j + u < m) dst[u] = row[u];
-        }
-      }
+      for (int u = 0; u < (int)sizeof(T); ++u)
+        reinterpret_cast<i32x4 *>(block + t.l16 * kPitch + 64 * g + 16 * t.q)[u] = reinterpret_cast<const i32x4 *>(row)[u];
     }
+    const int64_t i = i0 + 16 * (t.wb * Tile::kFragB + v);
+    T *dst = out + i * stride + j0;
+    if (width == 16) mx4_store_rows<T, kCols, 16>(block, kPitch, dst, stride, a.rows.n - i, b.rows.n - j0, t.lane);
+    else if (width == 4) mx4_store_rows<T, kCols, 4>(block, kPitch, dst, stride, a.rows.n - i, b.rows.n - j0, t.lane);
+    else mx4_store_rows<T, kCols, (int)sizeof(T)>(block, kPitch, dst, stride, a.rows.n - i, b.rows.n - j0, t.lane);
+    __builtin_amdgcn_wave_barrier();           // (a wavefront's LDS accesses are in order: the next rows may follow)
   }
 }
 
 typedef Mx4Tile<8, 4, 2, 4, false> Mx4Wide;       // 256 x 256
+typedef Mx4Tile<8, 2, 2, 4, false> Mx4Low;        // 256 columns x 128 rows: two workgroups a CU
 typedef Mx4Tile<4, 2, 2, 4, false> Mx4Narrow;     // 128 x 128
 
 // Up to this many rows of a the operands come straight from memory.
@@ -126,11 +162,12 @@ size_t mx4_product_bytes(const som_ctx *c, int64_t n, int64_t m) {
   return n <= kFewRows ? 0 : mx4_packed_bytes(n, blocks) + mx4_packed_bytes(m, blocks);
 }
 
-template <typename T, typename Tile>
+template <typename T, typename Tile, bool kStretch>
 static hipError_t product_tiles(som_ctx *c, Mx4Operand a, Mx4Operand b, T *out, int64_t stride) {
   const int blocks = mx4_blocks(c->dim);
   const int64_t tj = tiles(b.rows.n, Tile::kRowsA), ti = tiles(a.rows.n, Tile::kRowsB);
-  const bool vec = (uintptr_t)out % 16 == 0 && (stride * (int64_t)sizeof(T)) % 16 == 0;
+  const uintptr_t both = (uintptr_t)out | (uintptr_t)(a.rows.n > 1 ? stride * (int64_t)sizeof(T) : 0);
+  const int width = both % 16 == 0 ? 16 : both % 4 == 0 ? 4 : 2;
   const int64_t most = (1ll << 30) / tj > 0 ? (1ll << 30) / tj : 1;           // tile rows of a launch
   for (int64_t t0 = 0; t0 < ti; t0 += most) {
     const int64_t now = ti - t0 < most ? ti - t0 : most, i0 = t0 * Tile::kRowsB;
@@ -140,8 +177,8 @@ static hipError_t product_tiles(som_ctx *c, Mx4Operand a, Mx4Operand b, T *out, 
     part.rows.n = a.rows.n - i0;
     part.packed += (size_t)(i0 / 64) * ((blocks + 3) / 4) * 64;
     const dim3 grid((unsigned)(now * tj));
-    if (vec) hipLaunchKernelGGL((k_mx4_product<T, Tile, true>), grid, dim3(Tile::kThreads), 0, c->stream, part, b, blocks, c->zero16, out + i0 * stride, stride, (unsigned)tj);
-    else hipLaunchKernelGGL((k_mx4_product<T, Tile, false>), grid, dim3(Tile::kThreads), 0, c->stream, part, b, blocks, c->zero16, out + i0 * stride, stride, (unsigned)tj);
+    hipLaunchKernelGGL((k_mx4_product<T, Tile, kStretch>), grid, dim3(Tile::kThreads), 0, c->stream, part, b, blocks, c->zero16, out + i0 * stride, stride,
+                       (unsigned)tj, width);
   }
   return hipGetLastError();
 }
@@ -159,8 +196,11 @@ static hipError_t product(som_ctx *c, Mx4Rows a, Mx4Rows b, T *out, int64_t stri
   if (e == hipSuccess) e = launch_mx4_pack_scales(c->stream, b.scales, b.n, blocks, true, pb);
   if (e != hipSuccess) return e;
   const Mx4Operand oa = {a, pa}, ob = {b, pb};
-  if (tiles(a.n, Mx4Wide::kRowsB) * tiles(b.n, Mx4Wide::kRowsA) >= c->n_cu) return product_tiles<T, Mx4Wide>(c, oa, ob, out, stride);
-  return product_tiles<T, Mx4Narrow>(c, oa, ob, out, stride);
+  // Rows of up to 512 features are bound by the output: two workgroups a CU, one's stores beside the other's products (to bf16, us, wide / low
+  // tiles: 50,000 x 10,000 x 128 261 / 227, 256 295 / 254, 384 347 / 308, 20,000 x 10,000 x 500 151 / 146, 1,000 196 / 202).
+  if (tiles(a.n, Mx4Wide::kRowsB) * tiles(b.n, Mx4Wide::kRowsA) >= c->n_cu)
+    return blocks <= 16 ? product_tiles<T, Mx4Low, true>(c, oa, ob, out, stride) : product_tiles<T, Mx4Wide, false>(c, oa, ob, out, stride);
+  return product_tiles<T, Mx4Narrow, false>(c, oa, ob, out, stride);
 }
 
 hipError_t launch_mx4_product(som_ctx *c, Mx4Rows a, Mx4Rows b, void *out, int type, int64_t stride, void *scratch) {

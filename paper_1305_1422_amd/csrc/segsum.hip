@@ -1045,49 +1045,53 @@ hipError_t launch_accumulate_dense(som_ctx *c, const float *X, int64_t n, const 
 }
 
 // ---------------------------------------------------------------- microscaled 4-bit rows
-// A chunk's rows as in k_accumulate_dense, a word of eight elements per lane; the lanes that a row leaves over take further
+// A workgroup takes one chunk after the other (a map with few instances a node has more places for chunks than chunks, and to start a workgroup for each
+// place took longer than the sums).  A chunk's rows as in k_accumulate_dense, a word of eight elements per lane; the lanes that a row leaves over take further
 // rows of the chunk, and their sums are added in order.  A lane adds at most kChunkRows values of three significant bits in fp32, the lanes'
 // sums are added in fp64.
+constexpr int kMx4Fill = 16;              // workgroups per CU
 __global__ __launch_bounds__(256) void k_accumulate_mx4(Mx4Rows x, int dim, int words /* of a row */, int cols /* lanes of a row */,
                                                         const int32_t *__restrict__ perm, const int32_t *__restrict__ seg_off,
                                                         const int32_t *__restrict__ chunk_off, const int32_t *__restrict__ chunk_node,
                                                         int k, float *__restrict__ S, float *__restrict__ partial) {
   __shared__ int s_rows[kChunkRows];
   __shared__ float s_sum[256 * 8];
-  const int chunk = blockIdx.x;
-  if (chunk >= chunk_off[k]) return;
-  const int b = chunk_node[chunk];
-  const int first_chunk = chunk_off[b];
-  const int lo = seg_off[b] + (chunk - first_chunk) * kChunkRows;
-  const int hi = min(lo + kChunkRows, seg_off[b + 1]);
-  const int nrows = hi - lo;
-  if (threadIdx.x < nrows) s_rows[threadIdx.x] = perm[lo + threadIdx.x];
-  __syncthreads();
-  const bool single = (chunk_off[b + 1] - first_chunk) == 1;
-  float *dst = single ? S + (int64_t)b * dim : partial + (int64_t)chunk * dim;
   const int col = threadIdx.x % cols, slot = threadIdx.x / cols, slots = 256 / cols;
-  for (int q0 = 0; q0 < words; q0 += cols) {
-    const int q = q0 + col;
-    float a[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (q < words)
-      for (int r = slot; r < nrows; r += slots) {
-        const int64_t row = s_rows[r];
-        const unsigned word = reinterpret_cast<const unsigned *>(x.codes)[row * words + q];
-        const float scale = mx4_scale(x.scales[row * (words / 4) + q / 4]);
-        const mx_f32x2 p0 = mx4_pair<0>(word, scale), p1 = mx4_pair<1>(word, scale), p2 = mx4_pair<2>(word, scale), p3 = mx4_pair<3>(word, scale);
-        a[0] += p0[0]; a[1] += p0[1]; a[2] += p1[0]; a[3] += p1[1]; a[4] += p2[0]; a[5] += p2[1]; a[6] += p3[0]; a[7] += p3[1];
-      }
-    if (q0) __syncthreads();
-#pragma unroll
-    for (int u = 0; u < 8; ++u) s_sum[u * 256 + threadIdx.x] = a[u];
+  const int chunks = chunk_off[k];
+  for (int chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
+    const int b = chunk_node[chunk];
+    const int first_chunk = chunk_off[b];
+    const int lo = seg_off[b] + (chunk - first_chunk) * kChunkRows;
+    const int hi = min(lo + kChunkRows, seg_off[b + 1]);
+    const int nrows = hi - lo;
+    if (threadIdx.x < nrows) s_rows[threadIdx.x] = perm[lo + threadIdx.x];
     __syncthreads();
-    for (int t = threadIdx.x; t < 8 * cols; t += 256) {
-      const int u = t & 7, cc = t >> 3, c = (q0 + cc) * 8 + u;
-      if (c < dim) {
-        double sum = 0.0;
-        for (int s = 0; s < slots; ++s) sum += (double)s_sum[u * 256 + s * cols + cc];
-        dst[c] = (float)sum;
+    const bool single = (chunk_off[b + 1] - first_chunk) == 1;
+    float *dst = single ? S + (int64_t)b * dim : partial + (int64_t)chunk * dim;
+    for (int q0 = 0; q0 < words; q0 += cols) {
+      const int q = q0 + col;
+      float a[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+      if (q < words)
+        for (int r = slot; r < nrows; r += slots) {
+          const int64_t row = s_rows[r];
+          const unsigned word = reinterpret_cast<const unsigned *>(x.codes)[row * words + q];
+          const float scale = mx4_scale(x.scales[row * (words / 4) + q / 4]);
+          const mx_f32x2 p0 = mx4_pair<0>(word, scale), p1 = mx4_pair<1>(word, scale), p2 = mx4_pair<2>(word, scale), p3 = mx4_pair<3>(word, scale);
+          a[0] += p0[0]; a[1] += p0[1]; a[2] += p1[0]; a[3] += p1[1]; a[4] += p2[0]; a[5] += p2[1]; a[6] += p3[0]; a[7] += p3[1];
+        }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s_sum[u * 256 + threadIdx.x] = a[u];
+      __syncthreads();
+      const int used = min(slots, nrows);
+      for (int t = threadIdx.x; t < 8 * cols; t += 256) {
+        const int u = t & 7, cc = t >> 3, c = (q0 + cc) * 8 + u;
+        if (c < dim) {
+          double sum = 0.0;
+          for (int s = 0; s < used; ++s) sum += (double)s_sum[u * 256 + s * cols + cc];
+          dst[c] = (float)sum;
+        }
       }
+      __syncthreads();
     }
   }
 }
@@ -1100,7 +1104,7 @@ hipError_t launch_accumulate_mx4(som_ctx *c, Mx4Rows x, const int32_t *bmus) {
   const int words = 4 * mx4_blocks(c->dim);
   int cols = 4;
   while (cols < words && cols < 256) cols *= 2;
-  hipLaunchKernelGGL(k_accumulate_mx4, dim3((unsigned)max_chunks), dim3(256), 0, c->stream, x, c->dim, words, cols, c->sort_val[0],
+  hipLaunchKernelGGL(k_accumulate_mx4, dim3((unsigned)(max_chunks < kMx4Fill * c->n_cu ? max_chunks : kMx4Fill * c->n_cu)), dim3(256), 0, c->stream, x, c->dim, words, cols, c->sort_val[0],
                      c->seg_off, c->chunk_off, c->chunk_node, c->k, c->S, c->partial);
   return launch_combine(c, max_chunks);
 }
