@@ -172,32 +172,45 @@ def _ptr(t, dtype, name: str, allow_none: bool = False):
     return C.c_void_p(t.data_ptr())
 
 
+_TYPES = {}          # torch dtype -> SOM_FP32, SOM_FP16, SOM_BF16
+
+
 def _typed(t, name: str, columns: Optional[int] = None):
-    """(pointer, element type, row stride) of a matrix whose rows may lie apart."""
+    """(address, element type, row stride) of a matrix whose rows may lie apart."""
     import torch
-    types = {torch.float32: SOM_FP32, torch.float16: SOM_FP16, torch.bfloat16: SOM_BF16}
+    if not _TYPES:
+        _TYPES.update({torch.float32: SOM_FP32, torch.float16: SOM_FP16, torch.bfloat16: SOM_BF16})
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA/ROCm torch tensor (device memory)")
-    if t.dtype not in types:
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
         raise TypeError(f"{name} must have dtype float32, float16 or bfloat16, got {t.dtype}")
-    if t.dim() != 2:
+    shape = t.shape
+    if len(shape) != 2:
         raise TypeError(f"{name} must have two dimensions")
-    if columns is not None and t.shape[1] != columns:
-        raise ValueError(f"{name} must have {columns} columns, got {t.shape[1]}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    rows, wide = shape
+    if columns is not None and wide != columns:
+        raise ValueError(f"{name} must have {columns} columns, got {wide}")
+    step, one = t.stride()
+    if wide > 1 and one != 1:
         raise TypeError(f"{name} must be contiguous within its rows")
-    return C.c_void_p(t.data_ptr()), types[t.dtype], t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return t.data_ptr(), kind, step if rows > 1 else wide
 
 
 def _mx4(codes, scales, name: str):
-    """(codes pointer, scales pointer, rows) of microscaled 4-bit rows."""
+    """(address of the codes, of the scales, rows, blocks) of microscaled 4-bit rows."""
     import torch
-    pc, ps = _ptr(codes, torch.uint8, f"{name} codes"), _ptr(scales, torch.uint8, f"{name} scales")
-    if codes.dim() != 2 or scales.dim() != 2:
+    u8 = torch.uint8
+    for t, what in ((codes, "codes"), (scales, "scales")):
+        if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is u8 and t.is_contiguous()):
+            _ptr(t, u8, f"{name} {what}")          # raises
+    cs, ss = codes.shape, scales.shape
+    if len(cs) != 2 or len(ss) != 2:
         raise TypeError(f"{name} codes and scales must have two dimensions")
-    if codes.shape[0] != scales.shape[0] or codes.shape[1] != 16 * scales.shape[1]:
-        raise ValueError(f"{name} codes must be [n][16 B] where scales are [n][B], got {tuple(codes.shape)} and {tuple(scales.shape)}")
-    return pc, ps, codes.shape[0]
+    n, blocks = ss
+    if cs[0] != n or cs[1] != 16 * blocks:
+        raise ValueError(f"{name} codes must be [n][16 B] where scales are [n][B], got {tuple(cs)} and {tuple(ss)}")
+    return codes.data_ptr(), scales.data_ptr(), n, blocks
 
 
 def _check(ctx, rc: int):
@@ -294,52 +307,54 @@ def som_set_data_csr(ctx, indptr, indices, values) -> None:
 
 def som_mx4_quantize(ctx, rows, codes, scales) -> None:
     pr, kind, stride = _typed(rows, "rows")
-    pc, ps, n = _mx4(codes, scales, "the")
-    if n != rows.shape[0] or scales.shape[1] != (rows.shape[1] + 31) // 32:
+    pc, ps, n, blocks = _mx4(codes, scales, "the")
+    if n != rows.shape[0] or blocks != (rows.shape[1] + 31) // 32:
         raise ValueError("codes and scales do not fit the rows")
     _check(ctx, load().som_mx4_quantize(ctx, pr, kind, n, stride, pc, ps))
 
 
 def som_mx4_dequantize(ctx, codes, scales, rows) -> None:
     pr, kind, stride = _typed(rows, "rows")
-    pc, ps, n = _mx4(codes, scales, "the")
-    if n != rows.shape[0] or scales.shape[1] != (rows.shape[1] + 31) // 32:
+    pc, ps, n, blocks = _mx4(codes, scales, "the")
+    if n != rows.shape[0] or blocks != (rows.shape[1] + 31) // 32:
         raise ValueError("codes and scales do not fit the rows")
     _check(ctx, load().som_mx4_dequantize(ctx, pc, ps, n, pr, kind, stride))
 
 
 def som_mx4_product(ctx, codes_a, scales_a, codes_b, scales_b, out) -> None:
-    pa, sa, n = _mx4(codes_a, scales_a, "a's")
-    pb, sb, m = _mx4(codes_b, scales_b, "b's")
+    pa, sa, n, blocks_a = _mx4(codes_a, scales_a, "a's")
+    pb, sb, m, blocks_b = _mx4(codes_b, scales_b, "b's")
     po, kind, stride = _typed(out, "out", m)
-    if out.shape[0] != n or scales_a.shape[1] != scales_b.shape[1]:
+    if out.shape[0] != n or blocks_a != blocks_b:
         raise ValueError("a, b and out do not fit each other")
     _check(ctx, load().som_mx4_product(ctx, pa, sa, n, pb, sb, m, po, kind, stride))
 
 
 def som_bmus_mx4(ctx, codes, scales, node_codes, node_scales, bmus) -> None:
     import torch
-    pc, ps, n = _mx4(codes, scales, "the")
-    pw, sw, _ = _mx4(node_codes, node_scales, "the nodes'")
+    pc, ps, n, blocks = _mx4(codes, scales, "the")
+    pw, sw, _, node_blocks = _mx4(node_codes, node_scales, "the nodes'")
+    if blocks != node_blocks:
+        raise ValueError("instances and nodes do not fit each other")
     _check(ctx, load().som_bmus_mx4(ctx, pc, ps, n, pw, sw, _ptr(bmus, torch.int32, "bmus")))
 
 
 def som_update_mx4(ctx, codes, scales, bmus, codebook, radius: float, scale: float) -> None:
     import torch
-    pc, ps, n = _mx4(codes, scales, "the")
+    pc, ps, n, _ = _mx4(codes, scales, "the")
     _check(ctx, load().som_update_mx4(ctx, pc, ps, n, _ptr(bmus, torch.int32, "bmus"),
                                       _ptr(codebook, torch.float32, "codebook"), radius, scale))
 
 
 def som_train_epoch_mx4(ctx, codes, scales, codebook, radius: float, scale: float, bmus) -> None:
     import torch
-    pc, ps, n = _mx4(codes, scales, "the")
+    pc, ps, n, _ = _mx4(codes, scales, "the")
     _check(ctx, load().som_train_epoch_mx4(ctx, pc, ps, n, _ptr(codebook, torch.float32, "codebook"), radius, scale,
                                            _ptr(bmus, torch.int32, "bmus")))
 
 
 def som_set_data_mx4(ctx, codes, scales) -> None:
-    pc, ps, n = _mx4(codes, scales, "the")
+    pc, ps, n, _ = _mx4(codes, scales, "the")
     _check(ctx, load().som_set_data_mx4(ctx, pc, ps, n))
 
 

@@ -25,7 +25,7 @@ __device__ __forceinline__ bool mx4_better(double s, int i, double best, int arg
 
 struct Mx4Best {
   double score;
-  int node, pad;
+  int node;
 };
 
 __device__ __forceinline__ Mx4Best mx4_best_of_block(double best, int arg) {
@@ -38,30 +38,34 @@ __device__ __forceinline__ Mx4Best mx4_best_of_block(double best, int arg) {
     if (mx4_better(s, i, best, arg)) { best = s; arg = i; }
   }
   const int wave = threadIdx.x >> 6;
+  __syncthreads();                             // (it may have been called before)
   if ((threadIdx.x & 63) == 0) { s_best[wave] = best; s_arg[wave] = arg; }
   __syncthreads();
-  Mx4Best r = {s_best[0], s_arg[0], 0};
+  Mx4Best r = {s_best[0], s_arg[0]};
 #pragma unroll
   for (int w = 1; w < 4; ++w)
     if (mx4_better(s_best[w], s_arg[w], r.score, r.node)) { r.score = s_best[w]; r.node = s_arg[w]; }
   return r;
 }
 
-// blockIdx.y: the instance; blockIdx.x: a share of the nodes.  2^log_lanes lanes take a node.
-__global__ __launch_bounds__(256) void k_mx4_direct(Mx4Rows x, Mx4Rows w, int blocks, int log_lanes, Mx4Best *__restrict__ rec,
-                                                    int32_t *__restrict__ bmus) {
-  const int lanes = 1 << log_lanes, sub = threadIdx.x & (lanes - 1), per = 256 >> log_lanes;
+// blockIdx.y: the instance; blockIdx.x: a share of the nodes.  2^log_lanes lanes take a node.  The share that finishes last joins them: tickets
+// (one an instance, zero between calls) count them, records and tickets are read and written past the XCDs' own caches.
+__global__ __launch_bounds__(256) void k_mx4_direct(Mx4Rows x, Mx4Rows w, int blocks, int log_lanes, double *__restrict__ rec_score,
+                                                    int *__restrict__ rec_node, int *__restrict__ tickets, int32_t *__restrict__ bmus) {
+  __shared__ int s_last;
+  const int lanes = 1 << log_lanes, sub = threadIdx.x & (lanes - 1), per = 256 >> log_lanes, shares = gridDim.x;
   const int64_t row = blockIdx.y;
   const uint8_t *xs = x.scales + row * blocks;
   const i32x4 *xc = reinterpret_cast<const i32x4 *>(x.codes + row * blocks * 16);
   double best = -INFINITY;
   int arg = 0x7fffffff;
-  for (int64_t n0 = (int64_t)blockIdx.x * per; n0 < w.n; n0 += (int64_t)gridDim.x * per) {
+  for (int64_t n0 = (int64_t)blockIdx.x * per; n0 < w.n; n0 += (int64_t)shares * per) {
     const int64_t node = n0 + (threadIdx.x >> log_lanes);
     double s = 0.0;
     if (node < w.n) {
       const uint8_t *ws = w.scales + node * blocks;
       const i32x4 *wc = reinterpret_cast<const i32x4 *>(w.codes + node * blocks * 16);
+#pragma unroll 4
       for (int b = sub; b < blocks; b += lanes) {
         const int ex = xs[b], ew = ws[b];
         float xw, ww;
@@ -73,26 +77,37 @@ __global__ __launch_bounds__(256) void k_mx4_direct(Mx4Rows x, Mx4Rows w, int bl
     for (int o = 1; o < lanes; o <<= 1) s += __shfl_xor(s, o);
     if (sub == 0 && node < w.n && mx4_better(s, (int)node, best, arg)) { best = s; arg = (int)node; }
   }
-  const Mx4Best r = mx4_best_of_block(best, arg);
-  if (threadIdx.x == 0) {
-    if (gridDim.x == 1) bmus[row] = r.node == 0x7fffffff ? 0 : r.node;
-    else rec[row * gridDim.x + blockIdx.x] = r;
+  Mx4Best r = mx4_best_of_block(best, arg);
+  if (shares > 1) {
+    if (threadIdx.x == 0) {
+      __hip_atomic_store(&rec_score[row * shares + blockIdx.x], r.score, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(&rec_node[row * shares + blockIdx.x], r.node, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      // (the stores have reached memory before the ticket does; a release at this scope would write back the whole L2, 34 us for 2,000 workgroups
+      // instead of 6)
+      asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+      s_last = __hip_atomic_fetch_add(&tickets[row], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == shares - 1;
+    }
+    __syncthreads();
+    if (!s_last) return;
+    best = -INFINITY;
+    arg = 0x7fffffff;
+    for (int t = threadIdx.x; t < shares; t += 256) {
+      const double score = __hip_atomic_load(&rec_score[row * shares + t], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      const int node = __hip_atomic_load(&rec_node[row * shares + t], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (mx4_better(score, node, best, arg)) { best = score; arg = node; }
+    }
+    r = mx4_best_of_block(best, arg);
+    if (threadIdx.x == 0) __hip_atomic_store(&tickets[row], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
-}
-
-__global__ __launch_bounds__(256) void k_mx4_direct_join(const Mx4Best *__restrict__ rec, int shares, int32_t *__restrict__ bmus) {
-  const Mx4Best *mine = rec + (int64_t)blockIdx.x * shares;
-  double best = -INFINITY;
-  int arg = 0x7fffffff;
-  for (int t = threadIdx.x; t < shares; t += 256)
-    if (mx4_better(mine[t].score, mine[t].node, best, arg)) { best = mine[t].score; arg = mine[t].node; }
-  const Mx4Best r = mx4_best_of_block(best, arg);
-  if (threadIdx.x == 0) bmus[blockIdx.x] = r.node == 0x7fffffff ? 0 : r.node;
+  if (threadIdx.x == 0) bmus[row] = r.node == 0x7fffffff ? 0 : r.node;
 }
 
 // ---------------------------------------------------------------- direct search
-// Shares of the nodes per instance: enough workgroups to fill the chip, a pass over their lanes at least.
+// Shares of the nodes per instance: enough workgroups to fill the chip, a pass over their lanes at least; with more than one there are at most
+// kMx4Tickets instances.
 static int direct_shares(const som_ctx *c, int64_t n, int lanes) {
+  if (n > kMx4Tickets) return 1;
+  if (n >= 2 * c->n_cu) return 1;
   const int64_t all = ((int64_t)c->k * lanes + 255) / 256, want = (8 * (int64_t)c->n_cu + n - 1) / n;
   return (int)(want < all ? want : all);
 }
@@ -103,15 +118,15 @@ static int direct_lanes_log(int blocks) {
   return l;
 }
 
-static hipError_t search_direct(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int32_t *bmus) {
+static hipError_t search_direct(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int *tickets, int32_t *bmus) {
   const int blocks = mx4_blocks(c->dim), log_lanes = direct_lanes_log(blocks), shares = direct_shares(c, x.n, 1 << log_lanes);
-  Mx4Best *rec = static_cast<Mx4Best *>(scratch);
-  for (int64_t r0 = 0; r0 < x.n; r0 += 65535) {
+  double *score = static_cast<double *>(scratch);
+  int *node = reinterpret_cast<int *>(score + x.n * shares);
+  for (int64_t r0 = 0; r0 < x.n; r0 += 65535) {          // (one launch where there are several shares)
     const Mx4Rows part = {x.codes + r0 * blocks * 16, x.scales + r0 * blocks, x.n - r0 < 65535 ? x.n - r0 : 65535};
-    hipLaunchKernelGGL(k_mx4_direct, dim3(shares, (unsigned)part.n), dim3(256), 0, c->stream, part, w, blocks, log_lanes,
-                       rec + r0 * shares, bmus + r0);
+    hipLaunchKernelGGL(k_mx4_direct, dim3(shares, (unsigned)part.n), dim3(256), 0, c->stream, part, w, blocks, log_lanes, score, node, tickets,
+                       bmus + r0);
   }
-  if (shares > 1) hipLaunchKernelGGL(k_mx4_direct_join, dim3((unsigned)x.n), dim3(256), 0, c->stream, rec, shares, bmus);
   return hipGetLastError();
 }
 
@@ -135,11 +150,14 @@ struct Mx4Record {
 // The stream of nodes, 64 at a time (a unit): per step and group of 16 nodes their fragment (lane l: block l / 16 of node l % 16; 1 KB), then
 // per step the packed scales (mx4_tiles.hpp), then what the accumulators start from in the order of the nodes, rounded up to whole KB.
 __host__ __device__ constexpr int mx4_stream_bytes(int steps) { return steps * 4096 + ((steps + 1) * 256 + 1023) / 1024 * 1024; }
+// By group of 16 nodes besides, for k_mx4_resolve: per step the scales of its fragment, then its 16 starting values (in the stream those of a group share
+// lines with the others', 256 bytes a step: 126 us instead of ) .
+__host__ __device__ constexpr int mx4_group_bytes(int steps) { return (steps + 1) * 64; }
 
 // A workgroup takes 64 nodes at a time.  parts[blockIdx.x]: the largest |w|^2 it saw (fp64, rounded up to fp32; infinity if it overflows).
 // packed, init: the scales and starting values by themselves for k_mx4_search, or null.
 __global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int64_t padded, float *__restrict__ init, char *__restrict__ stream,
-                                                   int *__restrict__ packed, float *__restrict__ parts, Mx4Counts *__restrict__ counts) {
+                                                   char *__restrict__ by_group, int *__restrict__ packed, float *__restrict__ parts, Mx4Counts *__restrict__ counts) {
   __shared__ double s_norm[4][64];
   __shared__ float s_max[64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4, steps = (blocks + 3) / 4;
@@ -172,6 +190,7 @@ __global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int64_
         mx4_block_dots(x[t], x[t], xx, ww);
         norm[t] += e == 255 ? (double)NAN : (double)ww * mx4_pow2(2 * e - 254);
         *reinterpret_cast<i32x4 *>(mine + s * 4096 + (i >> 2) * 1024 + (16 * q + 4 * t + (i & 3)) * 16) = x[t];
+        by_group[(4 * g + (i >> 2)) * mx4_group_bytes(steps) + s * 64 + 16 * q + 4 * t + (i & 3)] = (char)e;
       }
       *reinterpret_cast<unsigned *>(mine + steps * 4096 + s * 256 + lane * 4) = v;
       if (packed && 64 * g < w.n) packed[(g * steps + s) * 64 + lane] = (int)v;
@@ -189,6 +208,7 @@ __global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int64_
       const bool usable = node < w.n && n2 == n2;      // a node with a NaN, and what is past the last one, can never win
       const float from = usable ? (float)(-0.5 * n2) : -INFINITY;
       if (init) init[node] = from;
+      *reinterpret_cast<float *>(by_group + node / 16 * mx4_group_bytes(steps) + steps * 64 + node % 16 * 4) = from;
       *reinterpret_cast<float *>(mine + steps * 4096 + steps * 256 + threadIdx.x * 4) = from;
       if (usable) most = fmaxf(most, __double2float_ru(n2));
     }
@@ -518,7 +538,7 @@ __device__ __forceinline__ double mx4_margin(double x2, float wmax2, int blocks)
 // together (1 KB a step in one piece of the stream).  A workgroup's instances that are left over take their places in the lists with one
 // addition: with one for every instance the additions, all to one word, would take as long as the rest.
 constexpr int kMx4Batch = 8;
-__global__ __launch_bounds__(256) void k_mx4_resolve(Mx4Rows x, const char *__restrict__ stream, int blocks, int turns,
+__global__ __launch_bounds__(256) void k_mx4_resolve(Mx4Rows x, const char *__restrict__ stream, const char *__restrict__ by_group, int blocks, int turns,
                                                      const Mx4Record *__restrict__ records, Mx4Cut cut, int halves, const float *__restrict__ parts,
                                                      int nparts, Mx4Counts *__restrict__ counts, int *__restrict__ list,
                                                      float *__restrict__ threshold, int *__restrict__ found, int *__restrict__ groups,
@@ -576,28 +596,27 @@ __global__ __launch_bounds__(256) void k_mx4_resolve(Mx4Rows x, const char *__re
 #pragma unroll 1
       for (int r0 = 0; r0 < 16; r0 += kMx4Batch) {
         mx_f32x4 acc[kMx4Batch];
-        const char *base[kMx4Batch];
-        int part[kMx4Batch];
+        const char *codes[kMx4Batch], *scales[kMx4Batch];
 #pragma unroll
         for (int r = 0; r < kMx4Batch; ++r) {
           const int g = __builtin_amdgcn_readlane(group, 16 * turn + r0 + r);
-          base[r] = stream + (g >> 2) * unit;
-          part[r] = g & 3;
-          acc[r] = *reinterpret_cast<const mx_f32x4 *>(base[r] + steps * 4352 + part[r] * 64 + q * 16);
+          codes[r] = stream + (g >> 2) * unit + (g & 3) * 1024;
+          scales[r] = by_group + (int64_t)g * mx4_group_bytes(steps);
+          acc[r] = *reinterpret_cast<const mx_f32x4 *>(scales[r] + steps * 64 + q * 16);
         }
         for (int s = 0; s < steps; ++s) {
           i32x4 c[kMx4Batch];
           int e[kMx4Batch];
 #pragma unroll
           for (int r = 0; r < kMx4Batch; ++r) {
-            c[r] = *reinterpret_cast<const i32x4 *>(base[r] + s * 4096 + part[r] * 1024 + lane * 16);
-            e[r] = *reinterpret_cast<const int *>(base[r] + steps * 4096 + s * 256 + part[r] * 16 + q * 64 + (l16 & 3) * 4);
+            c[r] = *reinterpret_cast<const i32x4 *>(codes[r] + s * 4096 + lane * 16);
+            e[r] = reinterpret_cast<const uint8_t *>(scales[r])[s * 64 + lane];
           }
           const int64_t b = tr * blocks + (4 * s + q < blocks ? 4 * s + q : blocks - 1);
           const i32x4 xc = *reinterpret_cast<const i32x4 *>(x.codes + b * 16);
           const int xs = x.scales[b];
 #pragma unroll
-          for (int r = 0; r < kMx4Batch; ++r) acc[r] = mx4_mfma<0, 0>(c[r], xc, acc[r], e[r] >> (8 * (l16 >> 2)), xs);
+          for (int r = 0; r < kMx4Batch; ++r) acc[r] = mx4_mfma<0, 0>(c[r], xc, acc[r], e[r], xs);
         }
 #pragma unroll
         for (int r = 0; r < kMx4Batch; ++r)
@@ -737,14 +756,19 @@ static Mx4Layout search_layout(const som_ctx *c, int64_t n) {
   return l;
 }
 
-// A direct search takes the vector units about 60 operations for 32 multiply-adds, and two launches; the other five.
+// Direct, or on the matrix cores?  What either takes, in us, fitted to measurements (instances, nodes, features, us matrix cores / direct: 1, 2,500,
+// 1,000 31 / 8; 100, 2,500, 1,000 55 / 33; 200 59 / 56; 400 65 / 103; 10,000, 400, 32 44 / 25; 20,000 47 / 45; 30, 40,000, 256 101 / 49; 100 113 / 136;
+// 3,000, 1,000, 128 32 / 48; 300, 300, 4,000 152 / 48; 100,000, 9, 100 35 / 117).
 static bool direct_pays(const som_ctx *c, int64_t n) {
-  return n * (double)c->k * mx4_blocks(c->dim) <= 8e6;
+  const double blocks = mx4_blocks(c->dim), steps = (mx4_blocks(c->dim) + 3) / 4;
+  const double direct = 8.0 + 4.2e-6 * n * c->k * blocks + 1.1e-3 * n;
+  const double matrix = 28.0 + 2.5 * steps + 6e-4 * c->k * steps + 2e-4 * n;
+  return direct <= matrix;
 }
 
 struct Mx4SearchScratch {
   float *init, *parts, *threshold;
-  char *stream;
+  char *stream, *by_group;
   int *packed_w, *packed_x, *list, *found, *groups;
   Mx4Counts *counts;
   Mx4Record *records;
@@ -765,6 +789,7 @@ static Mx4SearchScratch search_scratch(const som_ctx *c, int64_t n, const Mx4Lay
   m.parts = static_cast<float *>(take(kMx4NodeBlocks * 4));
   m.counts = static_cast<Mx4Counts *>(take(sizeof(Mx4Counts)));
   m.stream = static_cast<char *>(take((size_t)(l.padded / 64) * mx4_stream_bytes(steps)));
+  m.by_group = static_cast<char *>(take((size_t)(l.padded / 16) * mx4_group_bytes(steps)));
   m.packed_w = static_cast<int *>(take(l.sweep ? 0 : mx4_packed_bytes(c->k, blocks)));
   m.packed_x = static_cast<int *>(take(l.sweep ? 0 : mx4_packed_bytes(n, blocks)));
   m.records = static_cast<Mx4Record *>(take((size_t)l.records * N * sizeof(Mx4Record)));
@@ -779,7 +804,7 @@ static Mx4SearchScratch search_scratch(const som_ctx *c, int64_t n, const Mx4Lay
 size_t mx4_search_bytes(const som_ctx *c, int64_t n) {
   if (!direct_pays(c, n)) return search_scratch(c, n, search_layout(c, n), nullptr).bytes;
   const int shares = direct_shares(c, n, 1 << direct_lanes_log(mx4_blocks(c->dim)));
-  return shares > 1 ? (size_t)n * shares * sizeof(Mx4Best) : 0;
+  return shares > 1 ? (size_t)n * shares * (sizeof(double) + sizeof(int)) : 0;
 }
 
 template <int kT, bool kCollect>
@@ -814,20 +839,20 @@ static hipError_t launch_pass(som_ctx *c, Mx4Rows x, Mx4Rows w, const Mx4Layout 
   return hipGetLastError();
 }
 
-hipError_t launch_bmu_mx4(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int32_t *bmus) {
-  if (direct_pays(c, x.n)) return search_direct(c, x, w, scratch, bmus);
+hipError_t launch_bmu_mx4(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int *tickets, int32_t *bmus) {
+  if (direct_pays(c, x.n)) return search_direct(c, x, w, scratch, tickets, bmus);
   const Mx4Layout l = search_layout(c, x.n);
   const Mx4SearchScratch m = search_scratch(c, x.n, l, scratch);
   const int blocks = mx4_blocks(c->dim);
   const int parts = l.padded / 64 < kMx4NodeBlocks ? (int)(l.padded / 64) : kMx4NodeBlocks;
-  hipLaunchKernelGGL(k_mx4_nodes, dim3(parts), dim3(256), 0, c->stream, w, blocks, l.padded, l.sweep ? nullptr : m.init, m.stream,
+  hipLaunchKernelGGL(k_mx4_nodes, dim3(parts), dim3(256), 0, c->stream, w, blocks, l.padded, l.sweep ? nullptr : m.init, m.stream, m.by_group,
                      l.sweep ? nullptr : m.packed_w, m.parts, m.counts);
   hipError_t e = launch_pass<false>(c, x, w, l, m);
   if (e != hipSuccess) return e;
   // (fewer turns where there are not enough instances for as many workgroups as the chip holds)
   const int64_t by64 = (x.n + 63) / 64;
   const int turns = by64 >= 32 * (int64_t)c->n_cu ? 4 : by64 >= 16 * (int64_t)c->n_cu ? 2 : 1;
-  hipLaunchKernelGGL(k_mx4_resolve, dim3((unsigned)((by64 + turns - 1) / turns)), dim3(256), 0, c->stream, x, m.stream, blocks, turns,
+  hipLaunchKernelGGL(k_mx4_resolve, dim3((unsigned)((by64 + turns - 1) / turns)), dim3(256), 0, c->stream, x, m.stream, m.by_group, blocks, turns,
                      m.records, l.cut, l.sweep ? 1 : Mx4Sweep::kWavesA, m.parts, parts, m.counts, m.list, m.threshold, m.found, m.groups, bmus);
   e = launch_pass<true>(c, x, w, l, m);
   if (e != hipSuccess) return e;

@@ -511,7 +511,27 @@ int64_t group_table_entries(int k, int64_t n) {
 constexpr int kGatherThreads = 512;
 constexpr int kGatherMax = 8192;          // instances (their ids fit 16 bits of LDS each; 16 per thread)
 
-__global__ __launch_bounds__(kGatherThreads) void k_gather_sums(const float *__restrict__ X, const int32_t *__restrict__ bmus,
+// Element c of a row: of dense rows, of microscaled 4-bit ones.
+struct DenseColumn {
+  const float *col;
+  int dim;
+  __device__ __forceinline__ DenseColumn(const float *X, int dim_, int c) : col(X + c), dim(dim_) {}
+  __device__ __forceinline__ float operator()(int row) const { return col[(int64_t)row * dim]; }
+};
+struct Mx4Column {
+  const uint8_t *code, *scale;
+  int blocks;
+  bool high;
+  __device__ __forceinline__ Mx4Column(Mx4Rows x, int dim, int c)
+      : code(x.codes + c / 2), scale(x.scales + c / 32), blocks((dim + 31) / 32), high(c & 1) {}
+  __device__ __forceinline__ float operator()(int row) const {
+    const mx_f32x2 v = mx4_pair<0>(code[(int64_t)row * blocks * 16], mx4_scale(scale[(int64_t)row * blocks]));
+    return high ? v[1] : v[0];
+  }
+};
+
+template <typename Rows, typename Column>
+__global__ __launch_bounds__(kGatherThreads) void k_gather_sums(Rows X, const int32_t *__restrict__ bmus,
                                                                 int n, int k, int dim, int col_lanes,
                                                                 int32_t *__restrict__ counts, float *__restrict__ S,
                                                                 EpochTables tables, EpochSchedule schedule) {
@@ -564,12 +584,12 @@ __global__ __launch_bounds__(kGatherThreads) void k_gather_sums(const float *__r
   const int cl = tid % col_lanes, rl = tid / col_lanes;
   const int c = blockIdx.y * col_lanes + cl;
   const bool live = c < dim;
-  const float *col = X + (live ? c : 0);
+  const Column col(X, dim, live ? c : 0);
   double sum = 0.0;
   for (int r = rl; r < total; r += 8 * row_lanes) {
     float v[8];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) v[u] = col[(int64_t)s_list[min(r + u * row_lanes, total - 1)] * dim];      // (no branch: all in flight)
+    for (int u = 0; u < 8; ++u) v[u] = col(s_list[min(r + u * row_lanes, total - 1)]);      // (no branch: all in flight)
 #pragma unroll
     for (int u = 0; u < 8; ++u) sum += r + u * row_lanes < total ? (double)v[u] : 0.0;
   }
@@ -1013,19 +1033,22 @@ static hipError_t launch_combine(som_ctx *c, int64_t max_chunks) {
   return hipGetLastError();
 }
 
+template <typename Column, typename Rows>
+static hipError_t launch_gather(som_ctx *c, Rows X, int64_t n, const int32_t *bmus, const EpochSchedule *tables) {
+  int col_lanes = 16;
+  while (col_lanes < c->dim && col_lanes < 256) col_lanes *= 2;
+  EpochTables t{};
+  int64_t work = 0;
+  if (tables) t = epoch_tables(c, false, &work);
+  const int64_t more = (work + kGatherThreads - 1) / kGatherThreads;
+  const int blocks = c->k + (int)(more < 4 * c->n_cu ? more : 4 * c->n_cu);
+  hipLaunchKernelGGL((k_gather_sums<Rows, Column>), dim3(blocks, (c->dim + col_lanes - 1) / col_lanes), dim3(kGatherThreads), 0, c->stream, X,
+                     bmus, (int)n, c->k, c->dim, col_lanes, c->counts, c->S, t, tables ? *tables : EpochSchedule{});
+  return hipGetLastError();
+}
+
 hipError_t launch_accumulate_dense(som_ctx *c, const float *X, int64_t n, const int32_t *bmus, const EpochSchedule *tables) {
-  if (gather_pays(c, n)) {
-    int col_lanes = 16;
-    while (col_lanes < c->dim && col_lanes < 256) col_lanes *= 2;
-    EpochTables t{};
-    int64_t work = 0;
-    if (tables) t = epoch_tables(c, false, &work);
-    const int64_t more = (work + kGatherThreads - 1) / kGatherThreads;
-    const int blocks = c->k + (int)(more < 4 * c->n_cu ? more : 4 * c->n_cu);
-    hipLaunchKernelGGL(k_gather_sums, dim3(blocks, (c->dim + col_lanes - 1) / col_lanes), dim3(kGatherThreads), 0, c->stream, X,
-                       bmus, (int)n, c->k, c->dim, col_lanes, c->counts, c->S, t, tables ? *tables : EpochSchedule{});
-    return hipGetLastError();
-  }
+  if (gather_pays(c, n)) return launch_gather<DenseColumn>(c, X, n, bmus, tables);
   const hipError_t e = launch_group_by_bmu(c, bmus, n, kChunkRows);
   if (e != hipSuccess) return e;
   int64_t max_chunks = n / kChunkRows + (n < c->k ? n : c->k);
@@ -1096,7 +1119,8 @@ __global__ __launch_bounds__(256) void k_accumulate_mx4(Mx4Rows x, int dim, int 
   }
 }
 
-hipError_t launch_accumulate_mx4(som_ctx *c, Mx4Rows x, const int32_t *bmus) {
+hipError_t launch_accumulate_mx4(som_ctx *c, Mx4Rows x, const int32_t *bmus, const EpochSchedule *tables) {
+  if (gather_pays(c, x.n)) return launch_gather<Mx4Column>(c, x, x.n, bmus, tables);
   const hipError_t e = launch_group_by_bmu(c, bmus, x.n, kChunkRows);
   if (e != hipSuccess) return e;
   int64_t max_chunks = x.n / kChunkRows + (x.n < c->k ? x.n : c->k);

@@ -831,6 +831,23 @@ static int mx4_scratch(som_ctx *c, int which, size_t bytes, void **out) {
   return SOM_OK;
 }
 
+// Scratch of a search: its own, and the counters that start from zero.
+static int mx4_search_scratch(som_ctx *c, int64_t n, void **out) {
+  int rc = mx4_scratch(c, kMx4Search, mx4_search_bytes(c, n), out);
+  if (rc || c->mx4_tickets) return rc;
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(c->stream, &capture) != hipSuccess || capture != hipStreamCaptureStatusNone) {
+    (void)hipGetLastError();
+    return fail(c, SOM_ERR_STATE, "a recorded call needs scratch: make a call of this size before recording");
+  }
+  if (!dev_alloc_first(c, &c->mx4_tickets, (size_t)kMx4Tickets)) {
+    (void)hipGetLastError();
+    return fail(c, SOM_ERR_ALLOC, "cannot allocate the counters of the search of 4-bit rows");
+  }
+  SOM_LAUNCH(c, launch_fill_zero_u32(c->stream, c->mx4_tickets, kMx4Tickets));
+  return SOM_OK;
+}
+
 static int check_mx4(som_ctx *c, const uint8_t *codes, const uint8_t *scales, int64_t n) {
   if (!codes || !scales) return fail(c, SOM_ERR_INVALID_ARG, "codes or scales is NULL");
   if ((uintptr_t)codes % 16 != 0) return fail(c, SOM_ERR_INVALID_ARG, "codes must be aligned to 16 bytes");
@@ -848,12 +865,12 @@ static int check_typed(som_ctx *c, const void *rows, int type, int64_t n, int64_
 
 static int bmu_search_mx4(som_ctx *c, Mx4Rows x, Mx4Rows w, int32_t *bmus) {
   void *scratch = nullptr;
-  const int rc = mx4_scratch(c, kMx4Search, mx4_search_bytes(c, x.n), &scratch);
+  const int rc = mx4_search_scratch(c, x.n, &scratch);
   if (rc) return rc;
   c->two_level_n = 0;
   c->sub_tried = 0;
   StageTimer t(c, 0);
-  SOM_LAUNCH(c, launch_bmu_mx4(c, x, w, scratch, bmus));
+  SOM_LAUNCH(c, launch_bmu_mx4(c, x, w, scratch, c->mx4_tickets, bmus));
   return SOM_OK;
 }
 
@@ -862,16 +879,17 @@ static int ensure_mx4_epoch(som_ctx *c, int64_t n) {
   int rc = ensure_rows(c, n, true, false);
   void *p = nullptr;
   const size_t blocks = (size_t)mx4_blocks(c->dim);
-  if (!rc) rc = mx4_scratch(c, kMx4Search, mx4_search_bytes(c, n), &p);
+  if (!rc) rc = mx4_search_scratch(c, n, &p);
   if (!rc) rc = mx4_scratch(c, kMx4Codes, (size_t)c->k * blocks * 16, &p);
   if (!rc) rc = mx4_scratch(c, kMx4Scales, (size_t)c->k * blocks, &p);
   return rc;
 }
 
-static int update_mx4(som_ctx *c, Mx4Rows x, const int32_t *bmus, float *W) {
+// tables: the epoch whose tables are still to be written, or null.
+static int update_mx4(som_ctx *c, Mx4Rows x, const int32_t *bmus, float *W, const EpochSchedule *tables) {
   {
     StageTimer t(c, 3);
-    SOM_LAUNCH(c, launch_accumulate_mx4(c, x, bmus));
+    SOM_LAUNCH(c, launch_accumulate_mx4(c, x, bmus, tables));
   }
   StageTimer t(c, 4);
   SOM_LAUNCH(c, launch_smooth_and_divide(c, W));
@@ -879,7 +897,7 @@ static int update_mx4(som_ctx *c, Mx4Rows x, const int32_t *bmus, float *W) {
 }
 
 // The search of an epoch goes through the code book in the rows' own form.
-static int epoch_mx4(som_ctx *c, Mx4Rows x, float *W, int32_t *bmus) {
+static int epoch_mx4(som_ctx *c, Mx4Rows x, float *W, int32_t *bmus, const EpochSchedule *tables) {
   const Mx4Rows w = {static_cast<uint8_t *>(c->mx4_buf[kMx4Codes]), static_cast<uint8_t *>(c->mx4_buf[kMx4Scales]), c->k};
   {
     StageTimer t(c, 5);
@@ -887,7 +905,7 @@ static int epoch_mx4(som_ctx *c, Mx4Rows x, float *W, int32_t *bmus) {
                                       static_cast<uint8_t *>(c->mx4_buf[kMx4Scales])));
   }
   const int rc = bmu_search_mx4(c, x, w, bmus);
-  return rc ? rc : update_mx4(c, x, bmus, W);
+  return rc ? rc : update_mx4(c, x, bmus, W, tables);
 }
 
 // Nothing is registered, and nothing that was computed of a registered set holds.
@@ -1014,6 +1032,7 @@ void som_destroy(som_ctx *c) {
   dev_free(c->hot_counts); dev_free(c->hot_rank); dev_free(c->hot_cols); dev_free(c->hot_Wc); dev_free(c->hot_Wh);
   dev_free(c->hot_wscale);
   for (int b = 0; b < kMx4Bufs; ++b) dev_free(c->mx4_buf[b]);
+  dev_free(c->mx4_tickets);
   while (c->mx4_retired) {
     Mx4Retired *r = c->mx4_retired;
     c->mx4_retired = r->next;
@@ -1211,8 +1230,9 @@ int som_update_mx4(som_ctx *c, const uint8_t *codes, const uint8_t *scales, int6
   if (!rc) rc = check_epoch_scalars(c, radius, scale);
   if (!rc) rc = ensure_rows(c, n, true, false);
   if (rc) return rc;
-  SOM_LAUNCH(c, launch_epoch_params(c, epoch_schedule(c, 0, 1, radius, radius, scale, scale, SOM_COOL_LINEAR), false));
-  return update_mx4(c, Mx4Rows{codes, scales, n}, bmus, codebook);
+  const EpochSchedule q = epoch_schedule(c, 0, 1, radius, radius, scale, scale, SOM_COOL_LINEAR), *later = tables_later(c, n, false, q);
+  if (!later) SOM_LAUNCH(c, launch_epoch_params(c, q, false));
+  return update_mx4(c, Mx4Rows{codes, scales, n}, bmus, codebook, later);
 }
 
 int som_train_epoch_mx4(som_ctx *c, const uint8_t *codes, const uint8_t *scales, int64_t n, float *codebook, float radius,
@@ -1223,8 +1243,9 @@ int som_train_epoch_mx4(som_ctx *c, const uint8_t *codes, const uint8_t *scales,
   if (!rc) rc = check_epoch_scalars(c, radius, scale);
   if (!rc) rc = ensure_mx4_epoch(c, n);
   if (rc) return rc;
-  SOM_LAUNCH(c, launch_epoch_params(c, epoch_schedule(c, 0, 1, radius, radius, scale, scale, SOM_COOL_LINEAR), false));
-  return epoch_mx4(c, Mx4Rows{codes, scales, n}, codebook, bmus);
+  const EpochSchedule q = epoch_schedule(c, 0, 1, radius, radius, scale, scale, SOM_COOL_LINEAR), *later = tables_later(c, n, false, q);
+  if (!later) SOM_LAUNCH(c, launch_epoch_params(c, q, false));
+  return epoch_mx4(c, Mx4Rows{codes, scales, n}, codebook, bmus, later);
 }
 
 int som_set_data_mx4(som_ctx *c, const uint8_t *codes, const uint8_t *scales, int64_t n) {
@@ -1310,10 +1331,10 @@ int som_train_snapshots(som_ctx *c, int n_epochs, float radius0, float radiusN, 
   if (rc) return rc;
   for (int e = 0; e < n_epochs; ++e) {
     const EpochSchedule q = epoch_schedule(c, e, n_epochs, radius0, radiusN, scale0, scaleN, cooling);
-    const EpochSchedule *later = dense ? tables_later(c, c->d_n, !direct, q) : nullptr;
+    const EpochSchedule *later = dense || mx4 ? tables_later(c, c->d_n, !direct, q) : nullptr;
     if (!later) SOM_LAUNCH(c, launch_epoch_params(c, q, !direct));
     if (mx4) {
-      rc = epoch_mx4(c, c->d_mx4, codebook, bmus);
+      rc = epoch_mx4(c, c->d_mx4, codebook, bmus, later);
     } else if (dense) {
       rc = direct ? bmu_search_direct(c, c->d_data, c->d_n, codebook, bmus)
                   : bmu_search_dense(c, c->d_data, c->d_n, codebook, bmus, true, true,

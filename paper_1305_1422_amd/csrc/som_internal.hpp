@@ -132,6 +132,7 @@ struct Mx4Rows {
 };
 inline int mx4_blocks(int dim) { return (dim + 31) / 32; }
 enum { kMx4Search = 0, kMx4Codes = 1, kMx4Scales = 2, kMx4Bufs = 3 };
+constexpr int kMx4Tickets = 2048;         // instances that a direct search shares out, one counter each
 struct Mx4Retired {
   void *buf;
   Mx4Retired *next;
@@ -297,6 +298,7 @@ struct som_ctx {
   void *mx4_buf[som::kMx4Bufs];
   size_t mx4_cap[som::kMx4Bufs];
   som::Mx4Retired *mx4_retired;
+  int *mx4_tickets;       // [kMx4Tickets] zero between calls, lazily allocated
 
   // registered training set for som_train
   int data_kind;          // 0 none, 1 dense, 2 csr, 3 microscaled 4-bit
@@ -480,7 +482,7 @@ hipError_t launch_accumulate_dense(som_ctx *c, const float *X, int64_t n, const 
 hipError_t launch_accumulate_csr(som_ctx *c, const int64_t *indptr, const int32_t *indices,
                                  const float *values, int64_t n, int64_t nnz, const int32_t *bmus);   // -> S, counts
 
-hipError_t launch_accumulate_mx4(som_ctx *c, Mx4Rows x, const int32_t *bmus);                          // -> S, counts
+hipError_t launch_accumulate_mx4(som_ctx *c, Mx4Rows x, const int32_t *bmus, const EpochSchedule *tables);      // as launch_accumulate_dense
 
 // mx4.hip: type SOM_FP32, SOM_FP16 or SOM_BF16, stride in elements
 hipError_t launch_mx4_quantize(hipStream_t stream, const void *rows, int type, int64_t n, int64_t stride, int dim, uint8_t *codes,
@@ -491,7 +493,7 @@ size_t mx4_product_bytes(const som_ctx *c, int64_t n, int64_t m);      // its sc
 hipError_t launch_mx4_product(som_ctx *c, Mx4Rows a, Mx4Rows b, void *out, int type, int64_t stride, void *scratch);
 // bmu_mx4.hip
 size_t mx4_search_bytes(const som_ctx *c, int64_t n);       // scratch of a search of n rows among the c->k nodes
-hipError_t launch_bmu_mx4(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int32_t *bmus);
+hipError_t launch_bmu_mx4(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int *tickets, int32_t *bmus);
 
 // smooth.hip
 hipError_t launch_epoch_params(som_ctx *c, const EpochSchedule &q, bool search);
