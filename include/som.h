@@ -203,8 +203,8 @@ int som_mx4_dequantize(som_ctx *ctx, const uint8_t *codes, const uint8_t *scales
  *   codes_a, scales_a, n; codes_b, scales_b, m   the rows, of the context's dim, read only.
  *   out     device [n] rows of m elements of `type`, `stride` elements apart (>= m; any value if n = 1); what lies between
  *           the rows is left as it is.
- * Products of two blocks are exact; their sum is taken in fp32 (each addition cuts off below 2^-23 of its largest
- * term) and rounded once to the type.  A NaN block of either row makes the product NaN.
+ * Products of two blocks are exact; their sum is taken in fp32, in the order of the features, and rounded once to the
+ * type.  A NaN block of either row makes the product NaN.
  * Errors: as above, for out as for rows there.
  */
 int som_mx4_product(som_ctx *ctx, const uint8_t *codes_a, const uint8_t *scales_a, int64_t n, const uint8_t *codes_b,

@@ -719,6 +719,7 @@ __global__ __launch_bounds__(256) void k_mx4_exact(Mx4Rows x, Mx4Rows w, int blo
 struct Mx4Layout {
   bool sweep;              // k_mx4_sweep, else k_mx4_search
   Mx4Cut cut;
+  int at_once;             // workgroups a CU holds
   int grid, records;       // workgroups; records of an instance
   int64_t padded;          // nodes rounded up to whole stages
 };
@@ -749,6 +750,7 @@ static Mx4Layout search_layout(const som_ctx *c, int64_t n) {
   l.padded = l.cut.stages * nodes;
   const int64_t all = (n + l.cut.rows - 1) / l.cut.rows * l.cut.stages, most = at_once * (int64_t)c->n_cu;
   l.cut.per = (all + most - 1) / most;
+  l.at_once = at_once;
   l.grid = (int)((all + l.cut.per - 1) / l.cut.per);
   // pieces that a block's stages can be spread over
   const int64_t pieces = (l.cut.stages + l.cut.per - 2) / l.cut.per + 1;
@@ -817,7 +819,7 @@ static void launch_sweep(som_ctx *c, Mx4Rows x, const Mx4Layout &l, const Mx4Sea
 template <bool kCollect>
 static hipError_t launch_pass(som_ctx *c, Mx4Rows x, Mx4Rows w, const Mx4Layout &l, const Mx4SearchScratch &m) {
   const int blocks = mx4_blocks(c->dim);
-  const dim3 grid(kCollect ? (l.sweep ? 2 : 1) * c->n_cu : l.grid);
+  const dim3 grid(kCollect ? l.at_once * c->n_cu : l.grid);
   if (l.sweep) {
     switch ((blocks + 3) / 4) {
       case 1: launch_sweep<1, kCollect>(c, x, l, m, grid); break;

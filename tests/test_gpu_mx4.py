@@ -109,15 +109,24 @@ def test_round_trip_of_few_and_many_rows(n):
 @pytest.mark.parametrize("n,m,dim", [(1, 1, 1), (1, 70, 33), (3, 17, 128), (65, 63, 129), (64, 64, 32), (130, 300, 100), (257, 259, 512),
                                      (300, 70, 1000), (40, 513, 1500), (16, 16, 4096), (200, 200, 1), (4200, 4100, 96), (2000, 10000, 130)])
 def test_product(kind, n, m, dim):
-    """The instruction's four block sums and its addend are cut off at 2^-20 of their magnitudes at most, once for every 128
-    features, then there is one rounding to the type."""
+    """Exact sums of blocks added one after the other in fp32: half a step of at most the sum of the magnitudes for each block, then
+    one rounding to the type."""
     rng = np.random.default_rng(n + m + dim)
-    a, b = R.random_rows(rng, n, dim), R.random_rows(rng, m, dim)
+    check_product(kind, R.random_rows(rng, n, dim), R.random_rows(rng, m, dim), dim)
+
+
+@pytest.mark.parametrize("n,m,dim", [(70, 90, 100), (64, 64, 1000), (300, 130, 256)])
+def test_product_over_wide_scales(n, m, dim):
+    rng = np.random.default_rng(dim)
+    check_product("fp32", R.random_rows(rng, n, dim, 100, 130), R.random_rows(rng, m, dim, 115, 128), dim)
+
+
+def check_product(kind, a, b, dim):
     som = make(dim=dim)
     got = som.products_mx4(dev(a), dev(b), TYPES[kind]).double().cpu().numpy()
     va, vb = R.values(*a, dim), R.values(*b, dim)
     want, size = va @ vb.T, np.abs(va) @ np.abs(vb).T
-    tol = (dim + 127) // 128 * 2.0 ** -20 * size
+    tol = R.blocks(dim) * 2.0 ** -24 * (1 + 2.0 ** -20) * size
     tol = tol + HALF_STEP[kind] * (np.abs(want) + tol)
     over = np.abs(want) > 65504 * (1 + 2.0 ** -11) if kind == "fp16" else np.zeros_like(want, bool)
     assert np.all((np.abs(got - want) <= tol) | over)
@@ -147,7 +156,7 @@ def test_product_of_not_a_number_and_extremes():
         size = np.abs(R.values(*a, 200)) @ np.abs(R.values(*b, 200)).T
     rest = np.ones((20, 30), bool)
     rest[3], rest[:, 7], rest[4] = False, False, False
-    assert np.all(np.abs(got - want)[rest] <= (2 * 2.0 ** -20 * size + 2.0 ** -24 * np.abs(want) + 2.0 ** -120)[rest])
+    assert np.all(np.abs(got - want)[rest] <= (7 * 2.0 ** -24 * (1 + 2.0 ** -20) * size + 2.0 ** -24 * np.abs(want) + 2.0 ** -120)[rest])
     assert not np.isfinite(got[4][np.abs(want[4]) > 2.0 ** 129]).any()
     som.close()
 
@@ -484,7 +493,7 @@ def test_set_trained_stored_and_searched(oracle):
     b = som.bmus(mx, nodes=nodes)
     resp = som.products_mx4(mx, nodes).double().cpu().numpy()
     x, w = som.dequantize_mx4(mx).double().cpu().numpy(), som.dequantize_mx4(nodes).double().cpu().numpy()
-    assert np.abs(resp - x @ w.T).max() <= 2.0 ** -20 * (np.abs(x) @ np.abs(w).T).max() * 2
+    assert np.all(np.abs(resp - x @ w.T) <= 4 * 2.0 ** -24 * (np.abs(x) @ np.abs(w).T))      # three blocks and the rounding to fp32
     assert np.array_equal(b.cpu().numpy(), R.nearest(x, w))
     assert torch.equal(som.bmus(mx), b)
     dist, qe = som.bmu_distances(som.dequantize_mx4(mx), b)
