@@ -660,28 +660,29 @@ __global__ __launch_bounds__(256) void k_accumulate_dense(const float *__restric
 // Nodes with many chunks (early in training a few nodes hold most of the instances, thousands of chunks
 // each; one workgroup adding them one after the other took three times as long as computing them): every
 // group of kCombineGroup consecutive chunks of such a node is first added up, in place, into the group's
-// first chunk.  One workgroup per chunk slot; only the group leaders of large nodes do anything.
+// first chunk.  Only the group leaders of large nodes do anything; resident workgroups look for them.
 constexpr int kCombineGroup = 32;
 
 __global__ __launch_bounds__(256) void k_combine_groups(const int32_t *__restrict__ chunk_off,
                                                         const int32_t *__restrict__ chunk_node, int k, int dim,
                                                         float *__restrict__ partial) {
-  const int chunk = blockIdx.x;
-  if (chunk >= chunk_off[k]) return;
-  const int b = chunk_node[chunk];
-  const int c0 = chunk_off[b], nc = chunk_off[b + 1] - c0;
-  const int at = chunk - c0;
-  if (nc <= kCombineGroup || at % kCombineGroup != 0) return;
-  const int len = min(kCombineGroup, nc - at);
-  float *dst = partial + (int64_t)chunk * dim;
-  for (int c = blockIdx.y * blockDim.x + threadIdx.x; c < dim; c += gridDim.y * blockDim.x) {
-    double a[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    int t = 0;
-    for (; t + 8 <= len; t += 8)
+  const int chunks = chunk_off[k];
+  for (int chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
+    const int b = chunk_node[chunk];
+    const int c0 = chunk_off[b], nc = chunk_off[b + 1] - c0;
+    const int at = chunk - c0;
+    if (nc <= kCombineGroup || at % kCombineGroup != 0) continue;
+    const int len = min(kCombineGroup, nc - at);
+    float *dst = partial + (int64_t)chunk * dim;
+    for (int c = blockIdx.y * blockDim.x + threadIdx.x; c < dim; c += gridDim.y * blockDim.x) {
+      double a[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+      int t = 0;
+      for (; t + 8 <= len; t += 8)
 #pragma unroll
-      for (int u = 0; u < 8; ++u) a[u] += (double)dst[(int64_t)(t + u) * dim + c];
-    for (int u = 0; t < len; ++t, ++u) a[u] += (double)dst[(int64_t)t * dim + c];
-    dst[c] = (float)(((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7])));
+        for (int u = 0; u < 8; ++u) a[u] += (double)dst[(int64_t)(t + u) * dim + c];
+      for (int u = 0; t < len; ++t, ++u) a[u] += (double)dst[(int64_t)t * dim + c];
+      dst[c] = (float)(((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7])));
+    }
   }
 }
 
@@ -1026,7 +1027,7 @@ static hipError_t launch_combine(som_ctx *c, int64_t max_chunks) {
   if (ysplit > 16) ysplit = 16;
   const int cthreads = c->dim >= 256 ? 256 : (c->dim + 63) / 64 * 64;
   if (max_chunks > kCombineGroup)
-    hipLaunchKernelGGL(k_combine_groups, dim3((unsigned)max_chunks, ysplit), dim3(cthreads), 0, c->stream, c->chunk_off,
+    hipLaunchKernelGGL(k_combine_groups, dim3((unsigned)(max_chunks < 16 * c->n_cu ? max_chunks : 16 * c->n_cu), ysplit), dim3(cthreads), 0, c->stream, c->chunk_off,
                        c->chunk_node, c->k, c->dim, c->partial);
   hipLaunchKernelGGL(k_combine_chunks, dim3(c->k, ysplit), dim3(256), 0, c->stream, c->chunk_off, c->dim, c->partial,
                      c->S);
@@ -1068,53 +1069,65 @@ hipError_t launch_accumulate_dense(som_ctx *c, const float *X, int64_t n, const 
 }
 
 // ---------------------------------------------------------------- microscaled 4-bit rows
-// A workgroup takes one chunk after the other (a map with few instances a node has more places for chunks than chunks, and to start a workgroup for each
-// place took longer than the sums).  A chunk's rows as in k_accumulate_dense, a word of eight elements per lane; the lanes that a row leaves over take further
-// rows of the chunk, and their sums are added in order.  A lane adds at most kChunkRows values of three significant bits in fp32, the lanes'
-// sums are added in fp64.
+// A wavefront takes one chunk after the other (a map with few instances a node has more places for chunks than chunks, and to start a workgroup for
+// each place took longer than the sums; a chunk of one or two rows is a chain of four loads, so that many wavefronts have to be under way: 50,000
+// instances of 256 features on 40,000 nodes, us, a workgroup for each place / resident workgroups / resident wavefronts 33 / 23 / 20, with 16-byte
+// stores 12).  A lane has a word of
+// eight elements; the lanes that a row leaves over take further rows, and their sums are added in fp64.  A lane adds at most kChunkRows values of
+// two significant bits in fp32.
 constexpr int kMx4Fill = 16;              // workgroups per CU
 __global__ __launch_bounds__(256) void k_accumulate_mx4(Mx4Rows x, int dim, int words /* of a row */, int cols /* lanes of a row */,
                                                         const int32_t *__restrict__ perm, const int32_t *__restrict__ seg_off,
                                                         const int32_t *__restrict__ chunk_off, const int32_t *__restrict__ chunk_node,
                                                         int k, float *__restrict__ S, float *__restrict__ partial) {
-  __shared__ int s_rows[kChunkRows];
-  __shared__ float s_sum[256 * 8];
-  const int col = threadIdx.x % cols, slot = threadIdx.x / cols, slots = 256 / cols;
+  const int lane = threadIdx.x & 63, col = lane & (cols - 1), slot = lane / cols, slots = 64 / cols;
   const int chunks = chunk_off[k];
-  for (int chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
+  for (int chunk = blockIdx.x * 4 + (threadIdx.x >> 6); chunk < chunks; chunk += gridDim.x * 4) {
     const int b = chunk_node[chunk];
     const int first_chunk = chunk_off[b];
     const int lo = seg_off[b] + (chunk - first_chunk) * kChunkRows;
-    const int hi = min(lo + kChunkRows, seg_off[b + 1]);
-    const int nrows = hi - lo;
-    if (threadIdx.x < nrows) s_rows[threadIdx.x] = perm[lo + threadIdx.x];
-    __syncthreads();
+    const int nrows = min(kChunkRows, seg_off[b + 1] - lo);
+    const int mine = perm[lo + min(lane, nrows - 1)];
     const bool single = (chunk_off[b + 1] - first_chunk) == 1;
     float *dst = single ? S + (int64_t)b * dim : partial + (int64_t)chunk * dim;
-    for (int q0 = 0; q0 < words; q0 += cols) {
-      const int q = q0 + col;
+    for (int q0 = blockIdx.y * cols; q0 < words; q0 += gridDim.y * cols) {
+      const int q = min(q0 + col, words - 1);      // (lanes past the row read its last word)
       float a[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-      if (q < words)
-        for (int r = slot; r < nrows; r += slots) {
-          const int64_t row = s_rows[r];
-          const unsigned word = reinterpret_cast<const unsigned *>(x.codes)[row * words + q];
-          const float scale = mx4_scale(x.scales[row * (words / 4) + q / 4]);
-          const mx_f32x2 p0 = mx4_pair<0>(word, scale), p1 = mx4_pair<1>(word, scale), p2 = mx4_pair<2>(word, scale), p3 = mx4_pair<3>(word, scale);
-          a[0] += p0[0]; a[1] += p0[1]; a[2] += p1[0]; a[3] += p1[1]; a[4] += p2[0]; a[5] += p2[1]; a[6] += p3[0]; a[7] += p3[1];
+      for (int r0 = 0; r0 < nrows; r0 += 4 * slots) {
+        unsigned word[4];
+        float scale[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int r = r0 + u * slots + slot;
+          const int64_t row = __shfl(mine, min(r, nrows - 1));
+          word[u] = reinterpret_cast<const unsigned *>(x.codes)[row * words + q];
+          scale[u] = mx4_scale(x.scales[row * (words / 4) + q / 4]);
+          if (r >= nrows) { word[u] = 0; scale[u] = 1.f; }
         }
 #pragma unroll
-      for (int u = 0; u < 8; ++u) s_sum[u * 256 + threadIdx.x] = a[u];
-      __syncthreads();
-      const int used = min(slots, nrows);
-      for (int t = threadIdx.x; t < 8 * cols; t += 256) {
-        const int u = t & 7, cc = t >> 3, c = (q0 + cc) * 8 + u;
-        if (c < dim) {
-          double sum = 0.0;
-          for (int s = 0; s < used; ++s) sum += (double)s_sum[u * 256 + s * cols + cc];
-          dst[c] = (float)sum;
+        for (int u = 0; u < 4; ++u) {
+          const mx_f32x2 p0 = mx4_pair<0>(word[u], scale[u]), p1 = mx4_pair<1>(word[u], scale[u]);
+          const mx_f32x2 p2 = mx4_pair<2>(word[u], scale[u]), p3 = mx4_pair<3>(word[u], scale[u]);
+          a[0] += p0[0]; a[1] += p0[1]; a[2] += p1[0]; a[3] += p1[1]; a[4] += p2[0]; a[5] += p2[1]; a[6] += p3[0]; a[7] += p3[1];
         }
       }
-      __syncthreads();
+      double sum[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) sum[u] = (double)a[u];
+      if (nrows > 1)
+        for (int o = cols; o < 64; o <<= 1)
+#pragma unroll
+          for (int u = 0; u < 8; ++u) sum[u] += __shfl_xor(sum[u], o);
+      const int c = 8 * (q0 + col);
+      if (slot == 0 && dim % 4 == 0) {
+#pragma unroll
+        for (int u = 0; u < 8; u += 4)
+          if (c + u < dim) *reinterpret_cast<f32x4 *>(dst + c + u) = f32x4{(float)sum[u], (float)sum[u + 1], (float)sum[u + 2], (float)sum[u + 3]};
+      } else if (slot == 0) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+          if (c + u < dim) dst[c + u] = (float)sum[u];
+      }
     }
   }
 }
@@ -1127,8 +1140,10 @@ hipError_t launch_accumulate_mx4(som_ctx *c, Mx4Rows x, const int32_t *bmus, con
   if (max_chunks < 1) max_chunks = 1;
   const int words = 4 * mx4_blocks(c->dim);
   int cols = 4;
-  while (cols < words && cols < 256) cols *= 2;
-  hipLaunchKernelGGL(k_accumulate_mx4, dim3((unsigned)(max_chunks < kMx4Fill * c->n_cu ? max_chunks : kMx4Fill * c->n_cu)), dim3(256), 0, c->stream, x, c->dim, words, cols, c->sort_val[0],
+  while (cols < words && cols < 64) cols *= 2;
+  const int64_t fours = (max_chunks + 3) / 4;
+  const int passes = fours < 4 * c->n_cu ? (words + cols - 1) / cols : 1;      // few chunks: their columns are shared out
+  hipLaunchKernelGGL(k_accumulate_mx4, dim3((unsigned)(fours < kMx4Fill * c->n_cu ? fours : kMx4Fill * c->n_cu), passes), dim3(256), 0, c->stream, x, c->dim, words, cols, c->sort_val[0],
                      c->seg_off, c->chunk_off, c->chunk_node, c->k, c->S, c->partial);
   return launch_combine(c, max_chunks);
 }
