@@ -183,7 +183,7 @@ int som_set_data_csr(som_ctx *ctx, const int64_t *indptr, const int32_t *indices
  *
  * som_mx4_quantize - rows into this form.
  *   rows    device [n] rows of dim elements of `type` (SOM_FP32, SOM_FP16, SOM_BF16), `stride` elements apart
- *           (>= dim; any value if n = 1), read only.
+ *           (>= dim), read only.
  *   A block's scale is 2^(floor(log2 of its largest magnitude) - 2), at least 2^-127; its elements are divided by
  *   it and rounded to the nearest value, ties to the one with an even code; above 6 they become 6 (so the largest elements of a block may lose
  *   up to a quarter).  Zeros of either sign keep it.  A block with an infinity or a NaN becomes NaN (scale 255, codes 0); a block of
@@ -191,7 +191,7 @@ int som_set_data_csr(som_ctx *ctx, const int64_t *indptr, const int32_t *indices
  * som_mx4_dequantize - the values that rows of this form stand for, rounded once to `type` (exact for fp32 and
  *   bf16, but for magnitudes beyond their range; fp16 has subnormal values and infinity outside its own).
  *   rows    device, written: [n] rows of dim elements, `stride` apart; what lies between the rows is left as it is.
- * Errors of both: unknown type, stride < dim or >= 2^40 (n > 1), rows not aligned to their type -> SOM_ERR_INVALID_ARG.
+ * Errors of both: unknown type, stride < dim or >= 2^40, rows not aligned to their type -> SOM_ERR_INVALID_ARG.
  */
 int som_mx4_quantize(som_ctx *ctx, const void *rows, int type, int64_t n, int64_t stride, uint8_t *codes, uint8_t *scales);
 int som_mx4_dequantize(som_ctx *ctx, const uint8_t *codes, const uint8_t *scales, int64_t n, void *rows, int type,
@@ -201,7 +201,7 @@ int som_mx4_dequantize(som_ctx *ctx, const uint8_t *codes, const uint8_t *scales
  * som_mx4_product - the dot products of all pairs of two sets of microscaled 4-bit rows (the response of every node to every
  * instance, if b is a code book): out[i][j] = sum over the features of a_i and b_j.
  *   codes_a, scales_a, n; codes_b, scales_b, m   the rows, of the context's dim, read only.
- *   out     device [n] rows of m elements of `type`, `stride` elements apart (>= m; any value if n = 1); what lies between
+ *   out     device [n] rows of m elements of `type`, `stride` elements apart (>= m); what lies between
  *           the rows is left as it is.
  * Products of two blocks are exact; their sum is taken in fp32, in the order of the features, and rounded once to the
  * type.  A NaN block of either row makes the product NaN.
@@ -223,9 +223,11 @@ int som_mx4_product(som_ctx *ctx, const uint8_t *codes_a, const uint8_t *scales_
  * training set for som_train and som_train_snapshots, as for dense data.  The code book stays fp32; the search of an
  * epoch quantises it to this form first, so that an epoch's BMUs are those of som_bmus_mx4 against som_mx4_quantize of the incoming
  * code book.  The sums are those of the values that the rows stand for.
- * Scratch: 17/32 of a byte per weight of the code book (epochs), and per instance of a search up to 128 bytes.  It grows without
- * waiting: what it replaces is kept until som_destroy.  A call that is being recorded into a graph and needs more than
- * any call before it -> SOM_ERR_STATE, nothing enqueued.  (The update's own scratch is that of som_update_dense.)
+ * Scratch: the code book in this form for epochs, once more for searches; per instance of a search about 100 bytes, and 1/32 byte per feature
+ * of rows of more than 1,024; for products 1/32 byte per feature of either side.  It grows without waiting: what it replaces is kept until
+ * som_destroy, so that recorded searches and products keep theirs.  The update's own scratch is that of som_update_dense (a later call with
+ * more instances replaces it: record epochs after the largest).  A call that is being recorded into a graph and needs more scratch than
+ * any call before it -> SOM_ERR_STATE, nothing enqueued.
  * som_get_stats and som_two_level_stats do not cover these searches.
  */
 int som_bmus_mx4(som_ctx *ctx, const uint8_t *codes, const uint8_t *scales, int64_t n, const uint8_t *node_codes,

@@ -149,25 +149,28 @@ struct Mx4Record {
 
 // The stream of nodes, 64 at a time (a unit): per step and group of 16 nodes their fragment (lane l: block l / 16 of node l % 16; 1 KB), then
 // per step the packed scales (mx4_tiles.hpp), then what the accumulators start from in the order of the nodes, rounded up to whole KB.
-__host__ __device__ constexpr int mx4_stream_bytes(int steps) { return steps * 4096 + ((steps + 1) * 256 + 1023) / 1024 * 1024; }
+__host__ __device__ constexpr int64_t mx4_stream_bytes(int64_t steps) { return steps * 4096 + ((steps + 1) * 256 + 1023) / 1024 * 1024; }
 // By group of 16 nodes besides, for k_mx4_resolve: per step the scales of its fragment, then its 16 starting values (in the stream they share
 // their lines with those of other groups: 126 us instead of 118 for 1e6 instances of 128 features, 80 instead of 76 for 100,000 of 1,000).
-__host__ __device__ constexpr int mx4_group_bytes(int steps) { return (steps + 1) * 64; }
+__host__ __device__ constexpr int64_t mx4_group_bytes(int64_t steps) { return (steps + 1) * 64; }
 
 // A workgroup takes 64 nodes at a time.  parts[blockIdx.x]: the largest |w|^2 it saw (fp64, rounded up to fp32; infinity if it overflows).
 // packed, init: the scales and starting values by themselves for k_mx4_search, or null.
-__global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int64_t padded, float *__restrict__ init, char *__restrict__ stream,
+__global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int cols, int64_t padded, float *__restrict__ init, char *__restrict__ stream,
                                                    char *__restrict__ by_group, int *__restrict__ packed, float *__restrict__ parts, Mx4Counts *__restrict__ counts) {
   __shared__ double s_norm[4][64];
+  __shared__ unsigned s_same[4][16];
   __shared__ float s_max[64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4, steps = (blocks + 3) / 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
+  const int64_t steps = (blocks - 1) / 4 + 1;
   if (blockIdx.x == 0 && threadIdx.x == 0) *counts = Mx4Counts{0, 0};
   float most = 0.f;
   for (int64_t g = blockIdx.x; g < padded / 64; g += gridDim.x) {
-    char *mine = stream + g * (int64_t)mx4_stream_bytes(steps);
+    char *mine = stream + g * mx4_stream_bytes(steps);
     double norm[4] = {0, 0, 0, 0};
-    for (int s = wave; s < steps; s += 4) {
-      const int block = 4 * s + q;
+    unsigned same = 255;                       // bit t: like the node before it, so far; bit 4 + t: like the one a map row before it
+    for (int64_t s = wave; s < steps; s += 4) {
+      const int64_t block = 4 * s + q;
       unsigned v = 0;
       i32x4 x[4];
 #pragma unroll
@@ -176,6 +179,11 @@ __global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int64_
         const int64_t b = (node < w.n ? node : w.n - 1) * blocks + (block < blocks ? block : blocks - 1);
         x[t] = *reinterpret_cast<const i32x4 *>(w.codes + b * 16);
         v |= (unsigned)w.scales[b] << (8 * t);
+        // (a node without the other one is compared with itself, and told apart below)
+        const int64_t left = node >= 1 && node < w.n ? b - blocks : b, up = node >= cols && node < w.n ? b - (int64_t)cols * blocks : b;
+        const i32x4 dl = x[t] ^ *reinterpret_cast<const i32x4 *>(w.codes + left * 16), du = x[t] ^ *reinterpret_cast<const i32x4 *>(w.codes + up * 16);
+        if ((dl[0] | dl[1] | dl[2] | dl[3]) != 0 || w.scales[left] != w.scales[b]) same &= ~(1u << t);
+        if ((du[0] | du[1] | du[2] | du[3]) != 0 || w.scales[up] != w.scales[b]) same &= ~(16u << t);
       }
 #pragma unroll
       for (int t = 0; t < 4; ++t)
@@ -201,11 +209,18 @@ __global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int64_
       norm[t] += __shfl_xor(norm[t], 32);
       if (q == t) s_norm[wave][mx4_dealt(t, i)] = norm[t];
     }
+    same &= __shfl_xor(same, 16);
+    same &= __shfl_xor(same, 32);
+    if (q == 0) s_same[wave][i] = same;
     __syncthreads();
     if (threadIdx.x < 64) {
       const double n2 = ((s_norm[0][threadIdx.x] + s_norm[1][threadIdx.x]) + s_norm[2][threadIdx.x]) + s_norm[3][threadIdx.x];
       const int64_t node = 64 * g + threadIdx.x;
-      const bool usable = node < w.n && n2 == n2;      // a node with a NaN, and what is past the last one, can never win
+      // A node with a NaN, and what is past the last one, can never win; nor can one that is like a node before it, which takes the ties: while the
+      // radius is wide, whole regions of the map have the same 4-bit rows, and the lists of equally near groups would overflow.
+      const int at = threadIdx.x / 16 * 4 + threadIdx.x % 4, t = threadIdx.x % 16 / 4;
+      const unsigned like = (s_same[0][at] & s_same[1][at] & s_same[2][at] & s_same[3][at]) >> t;
+      const bool usable = node < w.n && n2 == n2 && !((like & 1) && node >= 1) && !((like & 16) && node >= cols);
       const float from = usable ? (float)(-0.5 * n2) : -INFINITY;
       if (init) init[node] = from;
       *reinterpret_cast<float *>(by_group + node / 16 * mx4_group_bytes(steps) + steps * 64 + node % 16 * 4) = from;
@@ -233,7 +248,7 @@ __global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int64_
 template <int kT, int kF, int kUnits, int kWavesPerSimd>
 struct Mx4SweepShape {
   static constexpr int F = kF, units = kUnits, rows = 64 * kF, waves = kWavesPerSimd;
-  static constexpr int unit = mx4_stream_bytes(kT), stage = kUnits * unit, rest = unit / 1024 - 4 * kT, lds = 2 * stage;
+  static constexpr int unit = (int)mx4_stream_bytes(kT), stage = kUnits * unit, rest = unit / 1024 - 4 * kT, lds = 2 * stage;
 };
 // F: as many as two wavefronts a SIMD leave registers for (one fewer with the lists to write); from 7 steps on a single wavefront with twice
 // as many (100,000 x 10,000, whole search, us, two wavefronts / one: 384 features 201 / 222, 512 262 / 284, 640 320 / 335, 768 383 / 409,
@@ -530,7 +545,7 @@ __global__ __launch_bounds__(512) void k_mx4_search(Mx4Operand x, Mx4Operand w, 
 __device__ __forceinline__ double mx4_margin(double x2, float wmax2, int blocks) {
   const double size = sqrt(36.0 * 32.0 * x2) * sqrt((double)wmax2) + 0.5 * (double)wmax2;
   if (!(size < 1e37)) return INFINITY;
-  return 2.0 * (((blocks + 3) / 4 + 1) * kMx4Delta * size + 1e-34 * blocks);
+  return 2.0 * (((blocks - 1) / 4 + 2) * kMx4Delta * size + 1e-34 * blocks);
 }
 
 // `turns` (1, 2 or 4) times 16 instances a wavefront: lane l has instance l % (16 turns) of them for what an instance needs once - its records, its
@@ -545,7 +560,7 @@ __global__ __launch_bounds__(256) void k_mx4_resolve(Mx4Rows x, const char *__re
                                                      int32_t *__restrict__ bmus) {
   __shared__ float s_max[4];
   __shared__ int s_count[2], s_base[2];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q = lane >> 4, steps = (blocks + 3) / 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q = lane >> 4, steps = (blocks - 1) / 4 + 1;
   const int64_t unit = mx4_stream_bytes(steps);
   float wmax2 = (int)threadIdx.x < nparts ? parts[threadIdx.x] : 0.f;
 #pragma unroll
@@ -609,7 +624,7 @@ __global__ __launch_bounds__(256) void k_mx4_resolve(Mx4Rows x, const char *__re
           int e[kMx4Batch];
 #pragma unroll
           for (int r = 0; r < kMx4Batch; ++r) {
-            c[r] = *reinterpret_cast<const i32x4 *>(codes[r] + s * 4096 + lane * 16);
+            c[r] = *reinterpret_cast<const i32x4 *>(codes[r] + (int64_t)s * 4096 + lane * 16);
             e[r] = reinterpret_cast<const uint8_t *>(scales[r])[s * 64 + lane];
           }
           const int64_t b = tr * blocks + (4 * s + q < blocks ? 4 * s + q : blocks - 1);
@@ -736,7 +751,7 @@ static void sweep_shape(int steps, int *rows, int *nodes, int *at_once) {
 
 static Mx4Layout search_layout(const som_ctx *c, int64_t n) {
   Mx4Layout l;
-  const int steps = (mx4_blocks(c->dim) + 3) / 4;
+  const int steps = (mx4_blocks(c->dim) - 1) / 4 + 1;
   int nodes = Mx4Sweep::kRowsA, at_once = 1;      // nodes of a stage, workgroups a CU holds
   l.sweep = steps <= kMx4SweepSteps;
   l.cut.rows = Mx4Sweep::kRowsB;
@@ -762,7 +777,7 @@ static Mx4Layout search_layout(const som_ctx *c, int64_t n) {
 // 1,000 31 / 8; 100, 2,500, 1,000 55 / 33; 200 59 / 56; 400 65 / 103; 10,000, 400, 32 44 / 25; 20,000 47 / 45; 30, 40,000, 256 101 / 49; 100 113 / 136;
 // 3,000, 1,000, 128 32 / 48; 300, 300, 4,000 152 / 48; 100,000, 9, 100 35 / 117).
 static bool direct_pays(const som_ctx *c, int64_t n) {
-  const double blocks = mx4_blocks(c->dim), steps = (mx4_blocks(c->dim) + 3) / 4;
+  const double blocks = mx4_blocks(c->dim), steps = (mx4_blocks(c->dim) - 1) / 4 + 1;
   const double direct = 8.0 + 2.6e-6 * n * c->k * (blocks + 0.6) + 8e-4 * n;
   const double matrix = 30.0 + 2.5 * steps + 6e-4 * c->k * steps + 2e-4 * n;
   return direct <= matrix;
@@ -778,7 +793,7 @@ struct Mx4SearchScratch {
 };
 
 static Mx4SearchScratch search_scratch(const som_ctx *c, int64_t n, const Mx4Layout &l, void *base) {
-  const int blocks = mx4_blocks(c->dim), steps = (blocks + 3) / 4;
+  const int blocks = mx4_blocks(c->dim), steps = (blocks - 1) / 4 + 1;
   const size_t N = (size_t)n;
   Mx4SearchScratch m;
   size_t at = 0;
@@ -821,7 +836,7 @@ static hipError_t launch_pass(som_ctx *c, Mx4Rows x, Mx4Rows w, const Mx4Layout 
   const int blocks = mx4_blocks(c->dim);
   const dim3 grid(kCollect ? l.at_once * c->n_cu : l.grid);
   if (l.sweep) {
-    switch ((blocks + 3) / 4) {
+    switch ((blocks - 1) / 4 + 1) {
       case 1: launch_sweep<1, kCollect>(c, x, l, m, grid); break;
       case 2: launch_sweep<2, kCollect>(c, x, l, m, grid); break;
       case 3: launch_sweep<3, kCollect>(c, x, l, m, grid); break;
@@ -847,7 +862,7 @@ hipError_t launch_bmu_mx4(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int *
   const Mx4SearchScratch m = search_scratch(c, x.n, l, scratch);
   const int blocks = mx4_blocks(c->dim);
   const int parts = l.padded / 64 < kMx4NodeBlocks ? (int)(l.padded / 64) : kMx4NodeBlocks;
-  hipLaunchKernelGGL(k_mx4_nodes, dim3(parts), dim3(256), 0, c->stream, w, blocks, l.padded, l.sweep ? nullptr : m.init, m.stream, m.by_group,
+  hipLaunchKernelGGL(k_mx4_nodes, dim3(parts), dim3(256), 0, c->stream, w, blocks, c->cols, l.padded, l.sweep ? nullptr : m.init, m.stream, m.by_group,
                      l.sweep ? nullptr : m.packed_w, m.parts, m.counts);
   hipError_t e = launch_pass<false>(c, x, w, l, m);
   if (e != hipSuccess) return e;

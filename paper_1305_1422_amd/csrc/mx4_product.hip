@@ -28,7 +28,7 @@ __global__ __launch_bounds__(256) void k_mx4_pack_scales(const uint8_t *__restri
 
 hipError_t launch_mx4_pack_scales(hipStream_t stream, const uint8_t *scales, int64_t n, int blocks, bool dealt, int *packed,
                                   const int *list, const int *count) {
-  const int steps = (blocks + 3) / 4;
+  const int steps = (blocks - 1) / 4 + 1;
   int64_t grid = ((n + 63) / 64 * steps * 64 + 255) / 256;
   if (grid > 4096) grid = 4096;
   hipLaunchKernelGGL(k_mx4_pack_scales, dim3((unsigned)grid), dim3(256), 0, stream, scales, n, blocks, steps, dealt ? 1 : 0, packed, list,
@@ -175,7 +175,7 @@ static hipError_t product_tiles(som_ctx *c, Mx4Operand a, Mx4Operand b, T *out, 
     part.rows.codes += i0 * blocks * 16;
     part.rows.scales += i0 * blocks;
     part.rows.n = a.rows.n - i0;
-    part.packed += (size_t)(i0 / 64) * ((blocks + 3) / 4) * 64;
+    part.packed += (size_t)(i0 / 64) * ((blocks - 1) / 4 + 1) * 64;
     const dim3 grid((unsigned)(now * tj));
     hipLaunchKernelGGL((k_mx4_product<T, Tile, kStretch>), grid, dim3(Tile::kThreads), 0, c->stream, part, b, blocks, c->zero16, out + i0 * stride, stride,
                        (unsigned)tj, width);

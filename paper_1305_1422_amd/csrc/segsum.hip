@@ -523,7 +523,7 @@ struct Mx4Column {
   int blocks;
   bool high;
   __device__ __forceinline__ Mx4Column(Mx4Rows x, int dim, int c)
-      : code(x.codes + c / 2), scale(x.scales + c / 32), blocks((dim + 31) / 32), high(c & 1) {}
+      : code(x.codes + c / 2), scale(x.scales + c / 32), blocks((dim - 1) / 32 + 1), high(c & 1) {}
   __device__ __forceinline__ float operator()(int row) const {
     const mx_f32x2 v = mx4_pair<0>(code[(int64_t)row * blocks * 16], mx4_scale(scale[(int64_t)row * blocks]));
     return high ? v[1] : v[0];

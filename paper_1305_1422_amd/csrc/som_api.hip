@@ -802,22 +802,36 @@ static int registered_csr_dense(som_ctx *c) {
 }
 
 // ---------------------------------------------------------------- microscaled 4-bit rows
-// Scratch buffer `which` of at least `bytes`.  Its predecessor stays allocated (each is at least twice the one before), so that nothing has
-// to wait and what is recorded in a graph keeps its memory.  A call that is being recorded allocates nothing.
+// Is the call being recorded into a graph?  It allocates nothing then.
+static bool recording(som_ctx *c) {
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(c->stream, &capture) == hipSuccess && capture == hipStreamCaptureStatusNone) return false;
+  (void)hipGetLastError();
+  return true;
+}
+
+static int fail_recording(som_ctx *c) {
+  return fail(c, SOM_ERR_STATE, "a recorded call needs scratch: make a call of this size before recording");
+}
+
+// Scratch buffer `which` of at least `bytes`.  Its predecessor stays allocated (each is at least twice the one before, memory allowing), so
+// that nothing has to wait and what is recorded in a graph keeps its memory.
 static int mx4_scratch(som_ctx *c, int which, size_t bytes, void **out) {
   if (bytes > c->mx4_cap[which]) {
-    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-    if (hipStreamIsCapturing(c->stream, &capture) != hipSuccess || capture != hipStreamCaptureStatusNone) {
-      (void)hipGetLastError();
-      return fail(c, SOM_ERR_STATE, "a recorded call needs scratch: make a call of this size before recording");
-    }
-    const size_t cap = bytes > 2 * c->mx4_cap[which] ? bytes : 2 * c->mx4_cap[which];
+    if (recording(c)) return fail_recording(c);
+    size_t cap = bytes > 2 * c->mx4_cap[which] ? bytes : 2 * c->mx4_cap[which];
     Mx4Retired *old = c->mx4_buf[which] ? (Mx4Retired *)malloc(sizeof(Mx4Retired)) : nullptr;
     char *buf = nullptr;
-    if ((c->mx4_buf[which] && !old) || !dev_alloc_first(c, &buf, cap)) {
+    bool ok = !c->mx4_buf[which] || old;
+    if (ok && cap > bytes && !dev_alloc(&buf, cap)) {
+      (void)hipGetLastError();
+      cap = bytes;
+    }
+    if (ok && !buf) ok = dev_alloc_first(c, &buf, cap);
+    if (!ok) {
       (void)hipGetLastError();
       free(old);
-      return fail(c, SOM_ERR_ALLOC, "cannot allocate %zu bytes of scratch for 4-bit rows", cap);
+      return fail(c, SOM_ERR_ALLOC, "cannot allocate %zu bytes of scratch for 4-bit rows", bytes);
     }
     if (old) {
       old->buf = c->mx4_buf[which];
@@ -833,19 +847,21 @@ static int mx4_scratch(som_ctx *c, int which, size_t bytes, void **out) {
 
 // Scratch of a search: its own, and the counters that start from zero.
 static int mx4_search_scratch(som_ctx *c, int64_t n, void **out) {
-  int rc = mx4_scratch(c, kMx4Search, mx4_search_bytes(c, n), out);
+  const int rc = mx4_scratch(c, kMx4Search, mx4_search_bytes(c, n), out);
   if (rc || c->mx4_tickets) return rc;
-  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(c->stream, &capture) != hipSuccess || capture != hipStreamCaptureStatusNone) {
-    (void)hipGetLastError();
-    return fail(c, SOM_ERR_STATE, "a recorded call needs scratch: make a call of this size before recording");
-  }
+  if (recording(c)) return fail_recording(c);
   if (!dev_alloc_first(c, &c->mx4_tickets, (size_t)kMx4Tickets)) {
     (void)hipGetLastError();
     return fail(c, SOM_ERR_ALLOC, "cannot allocate the counters of the search of 4-bit rows");
   }
   SOM_LAUNCH(c, launch_fill_zero_u32(c->stream, c->mx4_tickets, kMx4Tickets));
   return SOM_OK;
+}
+
+// Scratch of an update: that of dense data.
+static int mx4_update_scratch(som_ctx *c, int64_t n) {
+  if ((n > c->n_cap || !c->partial) && recording(c)) return fail_recording(c);
+  return ensure_rows(c, n, true, false);
 }
 
 static int check_mx4(som_ctx *c, const uint8_t *codes, const uint8_t *scales, int64_t n) {
@@ -859,7 +875,7 @@ static int check_typed(som_ctx *c, const void *rows, int type, int64_t n, int64_
   if (!rows) return fail(c, SOM_ERR_INVALID_ARG, "NULL pointer argument");
   if (type != SOM_FP32 && type != SOM_FP16 && type != SOM_BF16) return fail(c, SOM_ERR_INVALID_ARG, "unknown type %d", type);
   if ((uintptr_t)rows % (type == SOM_FP32 ? 4 : 2) != 0) return fail(c, SOM_ERR_INVALID_ARG, "rows are not aligned to their type");
-  if (n > 1 && (stride < width || stride >= (1ll << 40))) return fail(c, SOM_ERR_INVALID_ARG, "row stride below the row's length or above 2^40");
+  if (stride < width || stride >= (1ll << 40)) return fail(c, SOM_ERR_INVALID_ARG, "row stride below the row's length or above 2^40");
   return SOM_OK;
 }
 
@@ -876,7 +892,7 @@ static int bmu_search_mx4(som_ctx *c, Mx4Rows x, Mx4Rows w, int32_t *bmus) {
 
 // Scratch of an epoch on n rows, for what is enqueued before its first launch to be complete.
 static int ensure_mx4_epoch(som_ctx *c, int64_t n) {
-  int rc = ensure_rows(c, n, true, false);
+  int rc = mx4_update_scratch(c, n);
   void *p = nullptr;
   const size_t blocks = (size_t)mx4_blocks(c->dim);
   if (!rc) rc = mx4_search_scratch(c, n, &p);
@@ -1228,7 +1244,7 @@ int som_update_mx4(som_ctx *c, const uint8_t *codes, const uint8_t *scales, int6
   if (!codebook || !bmus) return fail(c, SOM_ERR_INVALID_ARG, "NULL pointer argument");
   int rc = check_mx4(c, codes, scales, n);
   if (!rc) rc = check_epoch_scalars(c, radius, scale);
-  if (!rc) rc = ensure_rows(c, n, true, false);
+  if (!rc) rc = mx4_update_scratch(c, n);
   if (rc) return rc;
   const EpochSchedule q = epoch_schedule(c, 0, 1, radius, radius, scale, scale, SOM_COOL_LINEAR), *later = tables_later(c, n, false, q);
   if (!later) SOM_LAUNCH(c, launch_epoch_params(c, q, false));

@@ -130,7 +130,7 @@ struct Mx4Rows {
   const uint8_t *codes, *scales;
   int64_t n;
 };
-inline int mx4_blocks(int dim) { return (dim + 31) / 32; }
+inline int mx4_blocks(int dim) { return (dim - 1) / 32 + 1; }
 enum { kMx4Search = 0, kMx4Codes = 1, kMx4Scales = 2, kMx4Bufs = 3 };
 constexpr int kMx4Tickets = 2048;         // instances that a direct search shares out, one counter each
 struct Mx4Retired {

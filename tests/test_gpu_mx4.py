@@ -222,6 +222,19 @@ def test_search_among_twins(dim):
     check_search(R.quantize(rng.standard_normal((n, dim))), R.quantize(np.concatenate([half, half[rng.permutation(k // 2)]])), dim)
 
 
+@pytest.mark.parametrize("rows,cols,dim", [(60, 70, 12), (1, 3000, 40), (70, 40, 1100), (64, 64, 64)])
+def test_search_among_regions(rows, cols, dim):
+    """Regions of the map whose nodes are alike, as a wide radius leaves them: the first node of the nearest region."""
+    rng = np.random.default_rng(rows + dim)
+    y, x = np.divmod(np.arange(rows * cols), cols)
+    region = (y // 9) * 100 + x // 11 + (x + 2 * y > 90) * 50
+    values = rng.standard_normal((region.max() + 1, dim))
+    w = values[region]
+    odd = rng.integers(0, rows * cols, 40)
+    w[odd] += 0.3 * rng.standard_normal((40, dim))
+    check_search(R.quantize(rng.standard_normal((3000, dim))), R.quantize(w), dim, rows)
+
+
 @pytest.mark.parametrize("n,k,dim", [(2, 100, 64), (2000, 1000, 64), (300, 300, 1200), (5000, 3000, 64), (1000, 500, 1200)])
 def test_search_on_a_coarse_grid(n, k, dim):
     """Small whole numbers: many nodes are equally near."""
@@ -455,7 +468,11 @@ def test_recording_a_call_that_needs_scratch_is_refused():
         with torch.cuda.graph(graph, stream=stream):
             with pytest.raises(capi.SomError) as err:
                 som.bmus(x, b, w)
-        assert err.value.code == capi.SOM_ERR_STATE
+            with pytest.raises(capi.SomError) as err2:
+                som.train_epoch(x, 2.0, bmus=b)
+            with pytest.raises(capi.SomError) as err3:
+                som.update(x, b, 2.0)
+        assert all(e.value.code == capi.SOM_ERR_STATE for e in (err, err2, err3))
         som.bmus(x, b, w)
         assert np.array_equal(b.cpu().numpy(), R.nearest(R.values(*host(x), dim), R.values(*host(w), dim)))
         som.close()
@@ -524,6 +541,7 @@ def test_refusals():
     assert L.som_mx4_quantize(ctx, px, 3, 10, 40, c, s) == bad and L.som_last_error(ctx)
     assert L.som_mx4_quantize(ctx, px, 0, 10, 39, c, s) == bad
     assert L.som_mx4_quantize(ctx, px, 0, 10, 1 << 40, c, s) == bad
+    assert L.som_mx4_quantize(ctx, px, 0, 1, 39, c, s) == bad and L.som_mx4_dequantize(ctx, c, s, 1, px, 0, 0) == bad
     assert L.som_mx4_quantize(ctx, px + 1, 0, 10, 40, c, s) == bad
     assert L.som_mx4_quantize(ctx, px, 0, 10, 40, c + 8, s) == bad
     assert L.som_mx4_quantize(ctx, None, 0, 10, 40, c, s) == bad
