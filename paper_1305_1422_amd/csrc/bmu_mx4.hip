@@ -12,8 +12,8 @@
 //                  margin of the largest, that is the node.  A wavefront has 16 instances; an instruction multiplies the 16 nodes of
 //                  one of them with all 16, a column of its result is of use, which is still a hundred times less than the vector units would need;
 //   k_mx4_search   again for the instances of which another group did: it lists the groups within the margin;
-//   k_mx4_exact    what is left, in fp64: the listed groups of these, the one group of the others; all nodes where there are more than kMx4List
-//                  groups, or where fp32 could overflow.
+//   k_mx4_exact    what is left, in fp64: the listed groups of these, the one group of the others; all nodes, shared out as in a direct
+//                  search, where there are more than kMx4List groups, or where fp32 could overflow.
 #include "mx4_tiles.hpp"
 
 namespace som {
@@ -48,18 +48,21 @@ __device__ __forceinline__ Mx4Best mx4_best_of_block(double best, int arg) {
   return r;
 }
 
-// blockIdx.y: the instance; blockIdx.x: a share of the nodes.  2^log_lanes lanes take a node.  The share that finishes last joins them: tickets
-// (one an instance, zero between calls) count them, records and tickets are read and written past the XCDs' own caches.
-__global__ __launch_bounds__(256) void k_mx4_direct(Mx4Rows x, Mx4Rows w, int blocks, int log_lanes, double *__restrict__ rec_score,
-                                                    int *__restrict__ rec_node, int *__restrict__ tickets, int32_t *__restrict__ bmus) {
+// What a workgroup does with one of `shares` shares of the nodes for an instance; 2^log_lanes lanes take a node.  The share that finishes last
+// joins them: ticket `at` (zero between calls) counts them, records at * shares .. and tickets are read and written past the XCDs' own caches.
+struct Mx4Joined {
+  double *score;
+  int *node, *tickets;
+};
+__device__ __forceinline__ void mx4_scan(const Mx4Rows &x, const Mx4Rows &w, int blocks, int log_lanes, int64_t row, int share, int shares, int at,
+                                         const Mx4Joined &join, int32_t *__restrict__ bmus) {
   __shared__ int s_last;
-  const int lanes = 1 << log_lanes, sub = threadIdx.x & (lanes - 1), per = 256 >> log_lanes, shares = gridDim.x;
-  const int64_t row = blockIdx.y;
+  const int lanes = 1 << log_lanes, sub = threadIdx.x & (lanes - 1), per = 256 >> log_lanes;
   const uint8_t *xs = x.scales + row * blocks;
   const i32x4 *xc = reinterpret_cast<const i32x4 *>(x.codes + row * blocks * 16);
   double best = -INFINITY;
   int arg = 0x7fffffff;
-  for (int64_t n0 = (int64_t)blockIdx.x * per; n0 < w.n; n0 += (int64_t)shares * per) {
+  for (int64_t n0 = (int64_t)share * per; n0 < w.n; n0 += (int64_t)shares * per) {
     const int64_t node = n0 + (threadIdx.x >> log_lanes);
     double s = 0.0;
     if (node < w.n) {
@@ -80,26 +83,31 @@ __global__ __launch_bounds__(256) void k_mx4_direct(Mx4Rows x, Mx4Rows w, int bl
   Mx4Best r = mx4_best_of_block(best, arg);
   if (shares > 1) {
     if (threadIdx.x == 0) {
-      __hip_atomic_store(&rec_score[row * shares + blockIdx.x], r.score, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      __hip_atomic_store(&rec_node[row * shares + blockIdx.x], r.node, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(&join.score[at * shares + share], r.score, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(&join.node[at * shares + share], r.node, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       // (the stores have reached memory before the ticket does; a release at this scope would write back the whole L2, 34 us for 2,000 workgroups
       // instead of 6)
       asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-      s_last = __hip_atomic_fetch_add(&tickets[row], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == shares - 1;
+      s_last = __hip_atomic_fetch_add(&join.tickets[at], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == shares - 1;
     }
     __syncthreads();
     if (!s_last) return;
     best = -INFINITY;
     arg = 0x7fffffff;
     for (int t = threadIdx.x; t < shares; t += 256) {
-      const double score = __hip_atomic_load(&rec_score[row * shares + t], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      const int node = __hip_atomic_load(&rec_node[row * shares + t], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      const double score = __hip_atomic_load(&join.score[at * shares + t], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      const int node = __hip_atomic_load(&join.node[at * shares + t], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       if (mx4_better(score, node, best, arg)) { best = score; arg = node; }
     }
     r = mx4_best_of_block(best, arg);
-    if (threadIdx.x == 0) __hip_atomic_store(&tickets[row], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (threadIdx.x == 0) __hip_atomic_store(&join.tickets[at], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   if (threadIdx.x == 0) bmus[row] = r.node == 0x7fffffff ? 0 : r.node;
+}
+
+// blockIdx.y: the instance; blockIdx.x: a share of the nodes.
+__global__ __launch_bounds__(256) void k_mx4_direct(Mx4Rows x, Mx4Rows w, int blocks, int log_lanes, Mx4Joined join, int32_t *__restrict__ bmus) {
+  mx4_scan(x, w, blocks, log_lanes, blockIdx.y, blockIdx.x, gridDim.x, blockIdx.y, join, bmus);
 }
 
 // ---------------------------------------------------------------- direct search
@@ -124,8 +132,8 @@ static hipError_t search_direct(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch,
   int *node = reinterpret_cast<int *>(score + x.n * shares);
   for (int64_t r0 = 0; r0 < x.n; r0 += 65535) {          // (one launch where there are several shares)
     const Mx4Rows part = {x.codes + r0 * blocks * 16, x.scales + r0 * blocks, x.n - r0 < 65535 ? x.n - r0 : 65535};
-    hipLaunchKernelGGL(k_mx4_direct, dim3(shares, (unsigned)part.n), dim3(256), 0, c->stream, part, w, blocks, log_lanes, score, node, tickets,
-                       bmus + r0);
+    hipLaunchKernelGGL(k_mx4_direct, dim3(shares, (unsigned)part.n), dim3(256), 0, c->stream, part, w, blocks, log_lanes,
+                       Mx4Joined{score, node, tickets}, bmus + r0);
   }
   return hipGetLastError();
 }
@@ -133,12 +141,14 @@ static hipError_t search_direct(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch,
 // ---------------------------------------------------------------- search on the matrix cores
 typedef Mx4Tile<8, 4, 2, 4, true> Mx4Sweep;      // 256 nodes x 256 instances
 
-constexpr int kMx4List = 16;            // groups an instance's list holds
+constexpr int kMx4List = 32;            // groups an instance's list holds (maps of a wide radius came to 23)
+constexpr int kMx4ScanBlocks = 2048;    // workgroups of the exact pass at most
 constexpr int kMx4NodeBlocks = 256;     // workgroups of the node pass at most
 constexpr float kMx4Lowest = -3.0e38f;  // below every score that counts
 
 struct Mx4Counts {
   int listed, single;      // instances to list groups of (slots from the front), with one group (slots from the back)
+  int whole;               // instances to be compared with all nodes (whole_list)
 };
 
 // Largest and second largest of the groups' maxima.
@@ -163,7 +173,7 @@ __global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int co
   __shared__ float s_max[64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
   const int64_t steps = (blocks - 1) / 4 + 1;
-  if (blockIdx.x == 0 && threadIdx.x == 0) *counts = Mx4Counts{0, 0};
+  if (blockIdx.x == 0 && threadIdx.x == 0) *counts = Mx4Counts{0, 0, 0};
   float most = 0.f;
   for (int64_t g = blockIdx.x; g < padded / 64; g += gridDim.x) {
     char *mine = stream + g * mx4_stream_bytes(steps);
@@ -281,9 +291,9 @@ __device__ __forceinline__ void mx4_in_order() {
 // kCollect as in k_mx4_search.
 template <int kT, bool kCollect>
 __global__ __launch_bounds__(256, (Mx4ShapeOf<kT, kCollect>::type::waves)) void k_mx4_sweep(Mx4Rows x, int blocks, const char *__restrict__ stream, Mx4Cut cut,
-                                                      Mx4Record *__restrict__ records, const Mx4Counts *__restrict__ counts,
+                                                      Mx4Record *__restrict__ records, Mx4Counts *__restrict__ counts,
                                                       const int *__restrict__ list, const float *__restrict__ threshold,
-                                                      int *__restrict__ found, int *__restrict__ groups) {
+                                                      int *__restrict__ found, int *__restrict__ groups, int *__restrict__ whole) {
   typedef typename Mx4ShapeOf<kT, kCollect>::type Shape;
   constexpr int kF = Shape::F, kUnits = Shape::units;
   constexpr bool kByF = kT == 1;
@@ -380,6 +390,7 @@ __global__ __launch_bounds__(256, (Mx4ShapeOf<kT, kCollect>::type::waves)) void 
         const int64_t slot = row0 + 16 * (wave * kF + f) + l16;
         const int place = atomicAdd(&found[slot], 1);
         if (place < kMx4List) groups[slot * kMx4List + place] = 4 * unit + q;
+        else if (place == kMx4List) whole[atomicAdd(&counts->whole, 1)] = list[slot];
       }
     };
     // kByF: the scores of two fragments of instances, the last ones' to begin with [1]; else those of all
@@ -459,9 +470,9 @@ __global__ __launch_bounds__(256, (Mx4ShapeOf<kT, kCollect>::type::waves)) void 
 template <bool kCollect>
 __global__ __launch_bounds__(512) void k_mx4_search(Mx4Operand x, Mx4Operand w, const float *__restrict__ init, int blocks,
                                                     const void *__restrict__ zero16, Mx4Cut cut, Mx4Record *__restrict__ records,
-                                                    const Mx4Counts *__restrict__ counts, const int *__restrict__ list,
+                                                    Mx4Counts *__restrict__ counts, const int *__restrict__ list,
                                                     const float *__restrict__ threshold, int *__restrict__ found,
-                                                    int *__restrict__ groups) {
+                                                    int *__restrict__ groups, int *__restrict__ whole) {
   typedef Mx4Sweep Tile;
   __shared__ __attribute__((aligned(16))) char smem[Tile::kLds];
   const int64_t n = kCollect ? counts->listed : x.rows.n, nb = (n + Tile::kRowsB - 1) / Tile::kRowsB;
@@ -510,6 +521,7 @@ __global__ __launch_bounds__(512) void k_mx4_search(Mx4Operand x, Mx4Operand w, 
               const int place = atomicAdd(&found[slot], 1);
               if (place < kMx4List)
                 groups[slot * kMx4List + place] = ((int)tile * (Tile::kRowsA / 64) + t.wa * (Tile::kFragA / 4) + g) * 4 + t.q;
+              else if (place == kMx4List) whole[atomicAdd(&counts->whole, 1)] = list[slot];
             }
           } else {
             second[v] = fmaxf(second[v], fminf(best[v], m));
@@ -557,20 +569,20 @@ __global__ __launch_bounds__(256) void k_mx4_resolve(Mx4Rows x, const char *__re
                                                      const Mx4Record *__restrict__ records, Mx4Cut cut, int halves, const float *__restrict__ parts,
                                                      int nparts, Mx4Counts *__restrict__ counts, int *__restrict__ list,
                                                      float *__restrict__ threshold, int *__restrict__ found, int *__restrict__ groups,
-                                                     int32_t *__restrict__ bmus) {
+                                                     int *__restrict__ whole, int32_t *__restrict__ bmus) {
   __shared__ float s_max[4];
-  __shared__ int s_count[2], s_base[2];
+  __shared__ int s_count[3], s_base[3];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q = lane >> 4, steps = (blocks - 1) / 4 + 1;
   const int64_t unit = mx4_stream_bytes(steps);
   float wmax2 = (int)threadIdx.x < nparts ? parts[threadIdx.x] : 0.f;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) wmax2 = fmaxf(wmax2, __shfl_xor(wmax2, o));
   if (lane == 0) s_max[wave] = wmax2;
-  if (threadIdx.x < 2) s_count[threadIdx.x] = 0;
+  if (threadIdx.x < 3) s_count[threadIdx.x] = 0;
   __syncthreads();
   wmax2 = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
   const int64_t row0 = ((int64_t)blockIdx.x * 4 + wave) * 16 * turns, row = row0 + (lane & (16 * turns - 1));
-  int what = 0, where = -1, place = 0;           // which list the lane's instance goes to, its place of this workgroup's; the group, -1: all nodes
+  int what = 0, where = -1, place = 0;           // which list the lane's instance goes to, its place of this workgroup's; its group
   float reach = 0.f;
   if (row0 < x.n) {
     const int64_t xr = row < x.n ? row : x.n - 1;
@@ -653,8 +665,7 @@ __global__ __launch_bounds__(256) void k_mx4_resolve(Mx4Rows x, const char *__re
       if (nan) {                                 // no finite distance to any node
         bmus[row] = 0;
       } else if (!(margin < INFINITY) || !(best > kMx4Lowest)) {
-        where = 1;
-        what = -1;
+        where = 2;
       } else if (second >= reach) {
         where = 0;
       } else if (near == 1) {
@@ -667,15 +678,17 @@ __global__ __launch_bounds__(256) void k_mx4_resolve(Mx4Rows x, const char *__re
     }
   }
   __syncthreads();
-  if (threadIdx.x < 2 && s_count[threadIdx.x] > 0)
-    s_base[threadIdx.x] = atomicAdd(threadIdx.x == 0 ? &counts->listed : &counts->single, s_count[threadIdx.x]);
+  if (threadIdx.x < 3 && s_count[threadIdx.x] > 0)
+    s_base[threadIdx.x] = atomicAdd(threadIdx.x == 0 ? &counts->listed : threadIdx.x == 1 ? &counts->single : &counts->whole, s_count[threadIdx.x]);
   __syncthreads();
-  if (where >= 0) {
+  if (where == 2) {
+    whole[s_base[2] + place] = (int)row;
+  } else if (where >= 0) {
     const int64_t slot = where == 0 ? s_base[0] + place : x.n - 1 - (s_base[1] + place);
     list[slot] = (int)row;
     threshold[slot] = reach;
-    found[slot] = where == 0 ? 0 : what < 0 ? kMx4List + 1 : 1;
-    if (where == 1 && what >= 0) groups[slot * kMx4List] = what;
+    found[slot] = where;
+    if (where == 1) groups[slot * kMx4List] = what;
   }
 }
 
@@ -683,18 +696,26 @@ __global__ __launch_bounds__(256) void k_mx4_resolve(Mx4Rows x, const char *__re
 template <int kEach>
 __global__ __launch_bounds__(256) void k_mx4_exact(Mx4Rows x, Mx4Rows w, int blocks, const Mx4Counts *__restrict__ counts,
                                                    const int *__restrict__ list, const int *__restrict__ found,
-                                                   const int *__restrict__ groups, int32_t *__restrict__ bmus) {
+                                                   const int *__restrict__ groups, const int *__restrict__ whole, int log_lanes,
+                                                   Mx4Joined join, int32_t *__restrict__ bmus) {
+  // those for all nodes first: they take longest
+  const int all = counts->whole, most = (int)gridDim.x / (all > 0 ? all : 1);
+  const int shares = all >= kMx4Tickets || most < 1 ? 1 : most < 64 ? most : 64;
+  for (int64_t job = blockIdx.x; job < (int64_t)all * shares; job += gridDim.x) {
+    mx4_scan(x, w, blocks, log_lanes, whole[job / shares], (int)(job % shares), shares, (int)(job / shares), join, bmus);
+    __syncthreads();
+  }
   const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
   const int64_t listed = counts->listed, total = listed + counts->single;
   for (int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); u < total; u += (int64_t)gridDim.x * 4) {
     const int64_t slot = u < listed ? u : x.n - 1 - (u - listed);
     const int64_t row = list[slot];
-    const bool all = found[slot] > kMx4List;
-    const int64_t ng = all ? (w.n + 15) / 16 : found[slot];
+    const int ng = found[slot];
+    if (ng > kMx4List) continue;               // (among those above)
     double best = -INFINITY;
     int arg = 0x7fffffff;
-    for (int64_t g = 0; g < ng; ++g) {
-      const int64_t node = 16 * (all ? g : (int64_t)groups[slot * kMx4List + g]) + l16, wr = node < w.n ? node : w.n - 1;
+    for (int g = 0; g < ng; ++g) {
+      const int64_t node = 16 * (int64_t)groups[slot * kMx4List + g] + l16, wr = node < w.n ? node : w.n - 1;
       double s = 0.0;
       for (int b0 = q; b0 < blocks; b0 += 4 * kEach) {
         i32x4 xc[kEach], wc[kEach];
@@ -786,7 +807,8 @@ static bool direct_pays(const som_ctx *c, int64_t n) {
 struct Mx4SearchScratch {
   float *init, *parts, *threshold;
   char *stream, *by_group;
-  int *packed_w, *packed_x, *list, *found, *groups;
+  int *packed_w, *packed_x, *list, *found, *groups, *whole, *joined_node;
+  double *joined_score;
   Mx4Counts *counts;
   Mx4Record *records;
   size_t bytes;
@@ -814,6 +836,9 @@ static Mx4SearchScratch search_scratch(const som_ctx *c, int64_t n, const Mx4Lay
   m.threshold = static_cast<float *>(take(N * 4));
   m.found = static_cast<int *>(take(N * 4));
   m.groups = static_cast<int *>(take(N * kMx4List * 4));
+  m.whole = static_cast<int *>(take(N * 4));
+  m.joined_score = static_cast<double *>(take(kMx4ScanBlocks * sizeof(double)));
+  m.joined_node = static_cast<int *>(take(kMx4ScanBlocks * sizeof(int)));
   m.bytes = at;
   return m;
 }
@@ -827,7 +852,7 @@ size_t mx4_search_bytes(const som_ctx *c, int64_t n) {
 template <int kT, bool kCollect>
 static void launch_sweep(som_ctx *c, Mx4Rows x, const Mx4Layout &l, const Mx4SearchScratch &m, dim3 grid) {
   hipLaunchKernelGGL((k_mx4_sweep<kT, kCollect>), grid, dim3(256), 0, c->stream, x, mx4_blocks(c->dim), m.stream, l.cut, m.records,
-                     m.counts, m.list, m.threshold, m.found, m.groups);
+                     m.counts, m.list, m.threshold, m.found, m.groups, m.whole);
 }
 
 // The pass over all instances (kCollect: over those that are listed, as many workgroups as fill the chip at most).
@@ -852,7 +877,7 @@ static hipError_t launch_pass(som_ctx *c, Mx4Rows x, Mx4Rows w, const Mx4Layout 
                                               kCollect ? &m.counts->listed : nullptr);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(k_mx4_search<kCollect>, grid, dim3(Mx4Sweep::kThreads), 0, c->stream, Mx4Operand{x, m.packed_x}, Mx4Operand{w, m.packed_w},
-                     m.init, blocks, c->zero16, l.cut, m.records, m.counts, m.list, m.threshold, m.found, m.groups);
+                     m.init, blocks, c->zero16, l.cut, m.records, m.counts, m.list, m.threshold, m.found, m.groups, m.whole);
   return hipGetLastError();
 }
 
@@ -870,13 +895,18 @@ hipError_t launch_bmu_mx4(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int *
   const int64_t by64 = (x.n + 63) / 64;
   const int turns = by64 >= 32 * (int64_t)c->n_cu ? 4 : by64 >= 16 * (int64_t)c->n_cu ? 2 : 1;
   hipLaunchKernelGGL(k_mx4_resolve, dim3((unsigned)((by64 + turns - 1) / turns)), dim3(256), 0, c->stream, x, m.stream, m.by_group, blocks, turns,
-                     m.records, l.cut, l.sweep ? 1 : Mx4Sweep::kWavesA, m.parts, parts, m.counts, m.list, m.threshold, m.found, m.groups, bmus);
+                     m.records, l.cut, l.sweep ? 1 : Mx4Sweep::kWavesA, m.parts, parts, m.counts, m.list, m.threshold, m.found, m.groups, m.whole, bmus);
   e = launch_pass<true>(c, x, w, l, m);
   if (e != hipSuccess) return e;
-  const int64_t most = (x.n + 3) / 4;
-  const dim3 grid((unsigned)(most < 8 * c->n_cu ? most : 8 * c->n_cu));
-  if (blocks > 8) hipLaunchKernelGGL(k_mx4_exact<4>, grid, dim3(256), 0, c->stream, x, w, blocks, m.counts, m.list, m.found, m.groups, bmus);
-  else hipLaunchKernelGGL(k_mx4_exact<1>, grid, dim3(256), 0, c->stream, x, w, blocks, m.counts, m.list, m.found, m.groups, bmus);
+  const int64_t wanted = (x.n + 3) / 4;
+  const dim3 grid((unsigned)(wanted < kMx4ScanBlocks ? wanted : kMx4ScanBlocks));
+  const Mx4Joined join = {m.joined_score, m.joined_node, tickets};
+  if (blocks > 8)
+    hipLaunchKernelGGL(k_mx4_exact<4>, grid, dim3(256), 0, c->stream, x, w, blocks, m.counts, m.list, m.found, m.groups, m.whole,
+                       direct_lanes_log(blocks), join, bmus);
+  else
+    hipLaunchKernelGGL(k_mx4_exact<1>, grid, dim3(256), 0, c->stream, x, w, blocks, m.counts, m.list, m.found, m.groups, m.whole,
+                       direct_lanes_log(blocks), join, bmus);
   return hipGetLastError();
 }
 
