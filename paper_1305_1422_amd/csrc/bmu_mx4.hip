@@ -9,8 +9,8 @@
 //   k_mx4_search   tiles of scores (mx4_tiles.hpp), never stored: per instance and group of 16 consecutive nodes - what a lane holds of a
 //                  tile - their maximum, of those the largest with its group and the largest of the other groups;
 //   k_mx4_resolve  where no other group comes within the margin: the 16 scores of the group again, and if one of them alone is within the
-//                  margin of the largest, that is the node.  A wavefront has 16 instances; an instruction multiplies the 16 nodes of
-//                  one of them with all 16, a column of its result is of use, which is still a hundred times less than the vector units would need;
+//                  margin of the largest, that is the node.  A wavefront has 16 instances, and an instruction multiplies the 16 nodes of a
+//                  group with all of them; columns of instances whose group it is not are of no use;
 //   k_mx4_search   again for the instances of which another group did: it lists the groups within the margin;
 //   k_mx4_exact    what is left, in fp64: the listed groups of these, the one group of the others; all nodes, shared out as in a direct
 //                  search, where there are more than kMx4List groups, or where fp32 could overflow.
@@ -560,135 +560,184 @@ __device__ __forceinline__ double mx4_margin(double x2, float wmax2, int blocks)
   return 2.0 * (((blocks - 1) / 4 + 2) * kMx4Delta * size + 1e-34 * blocks);
 }
 
-// `turns` (1, 2 or 4) times 16 instances a wavefront: lane l has instance l % (16 turns) of them for what an instance needs once - its records, its
-// margin, what becomes of it - and instance l % 16 of a turn for the products, for which the groups of kMx4Batch instances are fetched
-// together (1 KB a step in one piece of the stream).  A workgroup's instances that are left over take their places in the lists with one
-// addition: with one for every instance the additions, all to one word, would take as long as the rest.
-constexpr int kMx4Batch = 8;
-__global__ __launch_bounds__(256) void k_mx4_resolve(Mx4Rows x, const char *__restrict__ stream, const char *__restrict__ by_group, int blocks, int turns,
-                                                     const Mx4Record *__restrict__ records, Mx4Cut cut, int halves, const float *__restrict__ parts,
-                                                     int nparts, Mx4Counts *__restrict__ counts, int *__restrict__ list,
-                                                     float *__restrict__ threshold, int *__restrict__ found, int *__restrict__ groups,
-                                                     int *__restrict__ whole, int32_t *__restrict__ bmus) {
-  __shared__ float s_max[4];
+// A workgroup takes kEach instances, puts them in the order of their groups (more than 64 of them), and a wavefront multiplies 16 of them at a
+// time with each of the groups among them, kBatch in flight (1 KB a step in one piece of the stream).  What bounds it is the groups' way from
+// L2: 16 KB a step for 16 instances of as many groups.  See launch_resolve for the sizes.
+template <int kThreads, int kEach, int kBatch>
+__global__ __launch_bounds__(kThreads, 4) void k_mx4_resolve(Mx4Rows x, const char *__restrict__ stream, const char *__restrict__ by_group, int blocks,
+                                                      int ngroups, const Mx4Record *__restrict__ records, Mx4Cut cut, int halves,
+                                                      const float *__restrict__ parts, int nparts, Mx4Counts *__restrict__ counts,
+                                                      int *__restrict__ list, float *__restrict__ threshold, int *__restrict__ found,
+                                                      int *__restrict__ groups, int *__restrict__ whole, int32_t *__restrict__ bmus) {
+  constexpr bool kSort = kEach > 64;             // (of fewer there is nothing to gain)
+  __shared__ float s_best[kEach], s_second[kEach], s_inner[kEach];     // largest score, of the other groups, second one of the group
+  __shared__ int s_group[kEach], s_first[kEach];                       // the group, the largest score's place in it
+  __shared__ double s_x2[kEach];
+  __shared__ int s_order[kSort ? kEach : 1], s_from[kSort ? kThreads : 1], s_wave[kThreads / 64];
+  __shared__ float s_max[kThreads / 64];
   __shared__ int s_count[3], s_base[3];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q = lane >> 4, steps = (blocks - 1) / 4 + 1;
-  const int64_t unit = mx4_stream_bytes(steps);
+  const int64_t unit = mx4_stream_bytes(steps), row0 = (int64_t)blockIdx.x * kEach;
+  const int mine = x.n - row0 < kEach ? (int)(x.n - row0) : kEach;
   float wmax2 = (int)threadIdx.x < nparts ? parts[threadIdx.x] : 0.f;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) wmax2 = fmaxf(wmax2, __shfl_xor(wmax2, o));
   if (lane == 0) s_max[wave] = wmax2;
   if (threadIdx.x < 3) s_count[threadIdx.x] = 0;
+  if (kSort) s_from[threadIdx.x] = 0;
   __syncthreads();
-  wmax2 = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
-  const int64_t row0 = ((int64_t)blockIdx.x * 4 + wave) * 16 * turns, row = row0 + (lane & (16 * turns - 1));
-  int what = 0, where = -1, place = 0;           // which list the lane's instance goes to, its place of this workgroup's; its group
-  float reach = 0.f;
-  if (row0 < x.n) {
-    const int64_t xr = row < x.n ? row : x.n - 1;
-    float best = kMx4Lowest, second = kMx4Lowest;
-    int group = 0;
-    const int64_t block = xr / cut.rows, pieces = mx4_last_piece(cut, block) - mx4_first_piece(cut, block) + 1;
-    for (int64_t p = 0; p < pieces * halves; ++p) {
-      const Mx4Record r = records[p * x.n + xr];
-      second = fmaxf(fmaxf(second, r.second), fminf(best, r.best));
-      group = r.best > best ? r.group : group;
-      best = fmaxf(best, r.best);
-    }
-    double x2 = 0.0;                             // sum of the squares of the scales, NaN if one is
-    for (int turn = 0; turn < turns; ++turn) {
-      const int64_t tr = row0 + 16 * turn + l16 < x.n ? row0 + 16 * turn + l16 : x.n - 1;
-      double sum = 0.0;
-      for (int b0 = q; b0 < blocks; b0 += 16) {
-        int e[4];
+  wmax2 = s_max[0];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) e[u] = x.scales[tr * blocks + (b0 + 4 * u < blocks ? b0 + 4 * u : blocks - 1)];
+  for (int w = 1; w < kThreads / 64; ++w) wmax2 = fmaxf(wmax2, s_max[w]);
+  constexpr int kTurns = (kEach + kThreads - 1) / kThreads;
+  const int bits = 32 - __clz(ngroups - 1), most = 31 - __clz(kThreads), shift = bits > most ? bits - most : 0;
+  int bucket[kTurns], place[kTurns];
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-          if (b0 + 4 * u < blocks) sum += e[u] == 255 ? (double)NAN : mx4_pow2(2 * e[u] - 254);
+  for (int u = 0; u < kTurns; ++u) {
+    const int i = u * kThreads + threadIdx.x;
+    bucket[u] = place[u] = 0;
+    if (i < mine) {
+      const int64_t row = row0 + i, block = row / cut.rows, pieces = mx4_last_piece(cut, block) - mx4_first_piece(cut, block) + 1;
+      float best = kMx4Lowest, second = kMx4Lowest;
+      int group = 0;
+      for (int64_t p = 0; p < pieces * halves; ++p) {
+        const Mx4Record r = records[p * x.n + row];
+        second = fmaxf(fmaxf(second, r.second), fminf(best, r.best));
+        group = r.best > best ? r.group : group;
+        best = fmaxf(best, r.best);
       }
-      sum += __shfl_xor(sum, 16);
-      sum += __shfl_xor(sum, 32);
-      if ((q & (turns - 1)) == turn) x2 = sum;
-    }
-    const bool nan = x2 != x2;
-    const double margin = mx4_margin(x2, wmax2, blocks);
-    reach = __double2float_rd((double)best - margin);
-    int near = 0, first = 0;
-#pragma unroll 1
-    for (int turn = 0; turn < turns; ++turn) {
-      if (row0 + 16 * turn >= x.n) break;
-      const int64_t tr = row0 + 16 * turn + l16 < x.n ? row0 + 16 * turn + l16 : x.n - 1;
-      mx_f32x4 mine = {0.f, 0.f, 0.f, 0.f};      // scores of nodes 4 q .. of instance l16's group
-#pragma unroll 1
-      for (int r0 = 0; r0 < 16; r0 += kMx4Batch) {
-        mx_f32x4 acc[kMx4Batch];
-        const char *codes[kMx4Batch], *scales[kMx4Batch];
-#pragma unroll
-        for (int r = 0; r < kMx4Batch; ++r) {
-          const int g = __builtin_amdgcn_readlane(group, 16 * turn + r0 + r);
-          codes[r] = stream + (g >> 2) * unit + (g & 3) * 1024;
-          scales[r] = by_group + (int64_t)g * mx4_group_bytes(steps);
-          acc[r] = *reinterpret_cast<const mx_f32x4 *>(scales[r] + steps * 64 + q * 16);
-        }
-        for (int s = 0; s < steps; ++s) {
-          i32x4 c[kMx4Batch];
-          int e[kMx4Batch];
-#pragma unroll
-          for (int r = 0; r < kMx4Batch; ++r) {
-            c[r] = *reinterpret_cast<const i32x4 *>(codes[r] + (int64_t)s * 4096 + lane * 16);
-            e[r] = reinterpret_cast<const uint8_t *>(scales[r])[s * 64 + lane];
-          }
-          const int64_t b = tr * blocks + (4 * s + q < blocks ? 4 * s + q : blocks - 1);
-          const i32x4 xc = *reinterpret_cast<const i32x4 *>(x.codes + b * 16);
-          const int xs = x.scales[b];
-#pragma unroll
-          for (int r = 0; r < kMx4Batch; ++r) acc[r] = mx4_mfma<0, 0>(c[r], xc, acc[r], e[r], xs);
-        }
-#pragma unroll
-        for (int r = 0; r < kMx4Batch; ++r)
-          if (l16 == r0 + r) mine = acc[r];
-      }
-      const float limit = __shfl(reach, 16 * turn + l16);
-      int hits = 0, lowest = 16;
-#pragma unroll
-      for (int u = 3; u >= 0; --u)
-        if (mine[u] >= limit) { ++hits; lowest = 4 * q + u; }
-#pragma unroll
-      for (int o = 16; o < 64; o <<= 1) {
-        hits += __shfl_xor(hits, o);
-        lowest = min(lowest, __shfl_xor(lowest, o));
-      }
-      if ((q & (turns - 1)) == turn) { near = hits; first = lowest; }
-    }
-    if (lane < 16 * turns && row < x.n) {
-      if (nan) {                                 // no finite distance to any node
-        bmus[row] = 0;
-      } else if (!(margin < INFINITY) || !(best > kMx4Lowest)) {
-        where = 2;
-      } else if (second >= reach) {
-        where = 0;
-      } else if (near == 1) {
-        bmus[row] = 16 * group + first;
-      } else {
-        where = 1;
-        what = group;
-      }
-      if (where >= 0) place = atomicAdd(&s_count[where], 1);
+      s_best[i] = best;
+      s_second[i] = second;
+      s_group[i] = group;
+      bucket[u] = group >> shift;
+      if (kSort) place[u] = atomicAdd(&s_from[bucket[u]], 1);
     }
   }
   __syncthreads();
+  if (kSort) {
+    const int here = s_from[threadIdx.x];        // of a bucket; where it begins:
+    int sum = here;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int t = __shfl_up(sum, o);
+      if (lane >= o) sum += t;
+    }
+    if (lane == 63) s_wave[wave] = sum;
+    __syncthreads();
+    int before = 0;
+    for (int w = 0; w < wave; ++w) before += s_wave[w];
+    s_from[threadIdx.x] = before + sum - here;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kTurns; ++u)
+      if (u * kThreads + (int)threadIdx.x < mine) s_order[s_from[bucket[u]] + place[u]] = u * kThreads + threadIdx.x;
+    __syncthreads();
+  }
+#pragma unroll 1
+  for (int i0 = wave * 16; i0 < mine; i0 += kThreads / 4) {
+    const int nth = i0 + l16 < mine ? i0 + l16 : mine - 1, i = kSort ? s_order[nth] : nth;
+    const int64_t row = row0 + i;
+    const int group = s_group[i];
+    double x2 = 0.0;                             // sum of the squares of the scales, NaN if one is
+    mx_f32x4 mine4 = {0.f, 0.f, 0.f, 0.f};       // scores of nodes 4 q .. of instance l16's group
+    unsigned left = 0xffff;
+#pragma unroll 1
+    for (bool begin = true; left != 0; begin = false) {
+      int g[kBatch];
+      mx_f32x4 acc[kBatch];
+      const char *codes[kBatch], *scales[kBatch];
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r) {         // (the last group again where there are fewer)
+        g[r] = left != 0 || r == 0 ? __builtin_amdgcn_readlane(group, __builtin_ctz(left | 0x10000)) : g[r > 0 ? r - 1 : 0];
+        left &= ~(unsigned)__ballot(group == g[r]);
+        codes[r] = stream + (g[r] >> 2) * unit + (g[r] & 3) * 1024;
+        scales[r] = by_group + (int64_t)g[r] * mx4_group_bytes(steps);
+        acc[r] = *reinterpret_cast<const mx_f32x4 *>(scales[r] + steps * 64 + q * 16);
+      }
+      for (int s = 0; s < steps; ++s) {
+        i32x4 c[kBatch];
+        int e[kBatch];
+#pragma unroll
+        for (int r = 0; r < kBatch; ++r) {
+          c[r] = *reinterpret_cast<const i32x4 *>(codes[r] + (int64_t)s * 4096 + lane * 16);
+          e[r] = reinterpret_cast<const uint8_t *>(scales[r])[s * 64 + lane];
+        }
+        const int64_t b = row * blocks + (4 * s + q < blocks ? 4 * s + q : blocks - 1);
+        const i32x4 xc = *reinterpret_cast<const i32x4 *>(x.codes + b * 16);
+        const int xs = x.scales[b];
+#pragma unroll
+        for (int r = 0; r < kBatch; ++r) acc[r] = mx4_mfma<0, 0>(c[r], xc, acc[r], e[r], xs);
+        if (begin && 4 * s + q < blocks) x2 += xs == 255 ? (double)NAN : mx4_pow2(2 * xs - 254);
+      }
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r)
+        if (group == g[r]) mine4 = acc[r];
+    }
+    float b = mine4[0], second = kMx4Lowest;
+    int at = 4 * q;
+#pragma unroll
+    for (int u = 1; u < 4; ++u) {
+      second = fmaxf(second, fminf(b, mine4[u]));
+      at = mine4[u] > b ? 4 * q + u : at;
+      b = fmaxf(b, mine4[u]);
+    }
+#pragma unroll
+    for (int o = 16; o < 64; o <<= 1) {
+      const float ob = __shfl_xor(b, o), os = __shfl_xor(second, o);
+      const int oat = __shfl_xor(at, o);
+      second = fmaxf(fmaxf(second, os), fminf(b, ob));
+      at = ob > b ? oat : at;
+      b = fmaxf(b, ob);
+      x2 += __shfl_xor(x2, o);
+    }
+    if (q == 0 && i0 + l16 < mine) {
+      s_inner[i] = second;
+      s_first[i] = at;
+      s_x2[i] = x2;
+    }
+  }
+  __syncthreads();
+  int where[kTurns];
+  float reach[kTurns];
+#pragma unroll
+  for (int u = 0; u < kTurns; ++u) {
+    const int i = u * kThreads + threadIdx.x;
+    where[u] = -1;                               // which list it goes to; its place among this workgroup's
+    if (i < mine) {
+      const double x2 = s_x2[i], margin = mx4_margin(x2, wmax2, blocks);
+      const float best = s_best[i];
+      reach[u] = __double2float_rd((double)best - margin);
+      if (x2 != x2) {                            // no finite distance to any node
+        bmus[row0 + i] = 0;
+      } else if (!(margin < INFINITY) || !(best > kMx4Lowest)) {
+        where[u] = 2;
+      } else if (s_second[i] >= reach[u]) {
+        where[u] = 0;
+      } else if (s_inner[i] < reach[u]) {
+        bmus[row0 + i] = 16 * s_group[i] + s_first[i];
+      } else {
+        where[u] = 1;
+      }
+      if (where[u] >= 0) place[u] = atomicAdd(&s_count[where[u]], 1);
+    }
+  }
+  __syncthreads();
+  // (one addition a workgroup and list: with one for every instance the additions, all to one word, would take as long as the rest)
   if (threadIdx.x < 3 && s_count[threadIdx.x] > 0)
     s_base[threadIdx.x] = atomicAdd(threadIdx.x == 0 ? &counts->listed : threadIdx.x == 1 ? &counts->single : &counts->whole, s_count[threadIdx.x]);
   __syncthreads();
-  if (where == 2) {
-    whole[s_base[2] + place] = (int)row;
-  } else if (where >= 0) {
-    const int64_t slot = where == 0 ? s_base[0] + place : x.n - 1 - (s_base[1] + place);
-    list[slot] = (int)row;
-    threshold[slot] = reach;
-    found[slot] = where;
-    if (where == 1) groups[slot * kMx4List] = what;
+#pragma unroll
+  for (int u = 0; u < kTurns; ++u) {
+    const int i = u * kThreads + threadIdx.x;
+    if (where[u] == 2) {
+      whole[s_base[2] + place[u]] = (int)(row0 + i);
+    } else if (where[u] >= 0) {
+      const int64_t slot = where[u] == 0 ? s_base[0] + place[u] : x.n - 1 - (s_base[1] + place[u]);
+      list[slot] = (int)(row0 + i);
+      threshold[slot] = reach[u];
+      found[slot] = where[u];
+      if (where[u] == 1) groups[slot * kMx4List] = s_group[i];
+    }
   }
 }
 
@@ -881,6 +930,22 @@ static hipError_t launch_pass(som_ctx *c, Mx4Rows x, Mx4Rows w, const Mx4Layout 
   return hipGetLastError();
 }
 
+template <int kThreads, int kEach, int kBatch>
+static void launch_resolve_of(som_ctx *c, Mx4Rows x, const Mx4Layout &l, const Mx4SearchScratch &m, int parts, int32_t *bmus) {
+  hipLaunchKernelGGL((k_mx4_resolve<kThreads, kEach, kBatch>), dim3((unsigned)((x.n + kEach - 1) / kEach)), dim3(kThreads), 0, c->stream, x, m.stream,
+                     m.by_group, mx4_blocks(c->dim), (int)(l.padded / 16), m.records, l.cut, l.sweep ? 1 : Mx4Sweep::kWavesA, m.parts, parts, m.counts,
+                     m.list, m.threshold, m.found, m.groups, m.whole, bmus);
+}
+
+// The more instances are put in order the more of 16 have the same group, but fewer workgroups share the work: half as many as
+// CUs are enough (whole search, us, 64 / 512 / 2,048 instances a workgroup: 1e6 x 10,000 x 128 721 / 714 / 653, 200,000 x 2,500 x 1,000 361 / 327 / 340, 100,000
+// x 2,500 x 1,000 214 / 191 / 240, 50,000 x 2,500 x 128 56 / 56 / 64, 16,000 x 2,500 x 1,000 96 / 120 / 171).
+static void launch_resolve(som_ctx *c, Mx4Rows x, const Mx4Layout &l, const Mx4SearchScratch &m, int parts, int32_t *bmus) {
+  if (x.n >= 1024 * (int64_t)c->n_cu) launch_resolve_of<1024, 2048, 4>(c, x, l, m, parts, bmus);
+  else if (x.n >= 256 * (int64_t)c->n_cu) launch_resolve_of<1024, 512, 6>(c, x, l, m, parts, bmus);
+  else launch_resolve_of<256, 64, 8>(c, x, l, m, parts, bmus);
+}
+
 hipError_t launch_bmu_mx4(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int *tickets, int32_t *bmus) {
   if (direct_pays(c, x.n)) return search_direct(c, x, w, scratch, tickets, bmus);
   const Mx4Layout l = search_layout(c, x.n);
@@ -891,11 +956,7 @@ hipError_t launch_bmu_mx4(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int *
                      l.sweep ? nullptr : m.packed_w, m.parts, m.counts);
   hipError_t e = launch_pass<false>(c, x, w, l, m);
   if (e != hipSuccess) return e;
-  // (fewer turns where there are not enough instances for as many workgroups as the chip holds)
-  const int64_t by64 = (x.n + 63) / 64;
-  const int turns = by64 >= 32 * (int64_t)c->n_cu ? 4 : by64 >= 16 * (int64_t)c->n_cu ? 2 : 1;
-  hipLaunchKernelGGL(k_mx4_resolve, dim3((unsigned)((by64 + turns - 1) / turns)), dim3(256), 0, c->stream, x, m.stream, m.by_group, blocks, turns,
-                     m.records, l.cut, l.sweep ? 1 : Mx4Sweep::kWavesA, m.parts, parts, m.counts, m.list, m.threshold, m.found, m.groups, m.whole, bmus);
+  launch_resolve(c, x, l, m, parts, bmus);
   e = launch_pass<true>(c, x, w, l, m);
   if (e != hipSuccess) return e;
   const int64_t wanted = (x.n + 3) / 4;

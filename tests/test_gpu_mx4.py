@@ -295,6 +295,32 @@ def test_search_of_zeros(n):
     check_search(zero, R.quantize(np.zeros((k, dim))), dim)
 
 
+@pytest.mark.parametrize("n,k,dim,rows", [(65_537, 17_001, 40, 1), (66_000, 900, 300, 30), (90_001, 400, 1_100, 1), (262_145, 2_500, 64, 50),
+                                          (270_000, 17_000, 33, 10), (300_007, 300, 200, 3)])
+def test_search_of_many(n, k, dim, rows):
+    """As many instances as are put in order among one another, with ties, copies, NaN and zeros among them."""
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    w, x = torch.randn(k, dim, generator=gen, device="cuda"), torch.randn(n, dim, generator=gen, device="cuda")
+    w[5::7] = w[2::7][:len(w[5::7])].clone()                # equal nodes in other groups,
+    w[16:24] = w[24:32]                                     # and in the same one
+    x[100:40_000] = w[torch.randint(0, k, (39_900,), generator=gen, device="cuda")]
+    x[40_000:50_000] = w[33] + 0.01 * x[40_000:50_000]      # all of one node
+    x[50_000:50_100] = 0.0
+    x[n - 5:, 1] = float("nan")
+    som = make(rows, k // rows, dim)
+    x, w = som.quantize_mx4(x), som.quantize_mx4(w)
+    got = som.bmus(x, nodes=w).long()
+    xv, wv = som.dequantize_mx4(x).double(), som.dequantize_mx4(w).double()
+    half, at = 0.5 * (wv * wv).sum(1), torch.arange(k, device="cuda")
+    for i in range(0, n, 8192):
+        part = xv[i:i + 8192]
+        s = part @ wv.T - half                              # (exact: numbers of a kind, few bits)
+        want = torch.where(s == s.max(1, keepdim=True).values, at, k).min(1).values
+        want[part.isnan().any(1)] = 0
+        assert torch.equal(got[i:i + 8192], want), i
+    som.close()
+
+
 def test_searches_of_different_sizes_follow_one_another():
     """Scratch that grows and is reused: small after large, large after small, on one map."""
     rng = np.random.default_rng(15)
