@@ -922,8 +922,8 @@ static hipError_t launch_pass(som_ctx *c, Mx4Rows x, Mx4Rows w, const Mx4Layout 
     }
     return hipGetLastError();
   }
-  const hipError_t e = launch_mx4_pack_scales(c->stream, x.scales, x.n, blocks, false, m.packed_x, kCollect ? m.list : nullptr,
-                                              kCollect ? &m.counts->listed : nullptr);
+  const hipError_t e = launch_mx4_pack_scales(c->stream, blocks, Mx4Unpacked{x.scales, x.n, false, m.packed_x, kCollect ? m.list : nullptr,
+                                                                             kCollect ? &m.counts->listed : nullptr});
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(k_mx4_search<kCollect>, grid, dim3(Mx4Sweep::kThreads), 0, c->stream, Mx4Operand{x, m.packed_x}, Mx4Operand{w, m.packed_w},
                      m.init, blocks, c->zero16, l.cut, m.records, m.counts, m.list, m.threshold, m.found, m.groups, m.whole);

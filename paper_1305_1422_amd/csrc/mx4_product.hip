@@ -6,12 +6,16 @@
 namespace som {
 
 // ---------------------------------------------------------------- scales
-__global__ __launch_bounds__(256) void k_mx4_pack_scales(const uint8_t *__restrict__ scales, int64_t n, int blocks, int steps, int dealt,
-                                                         int *__restrict__ packed, const int *__restrict__ list,
-                                                         const int *__restrict__ count) {
-  if (count) n = *count;
-  const int64_t words = (n + 63) / 64 * steps * 64;
-  for (int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x; w < words; w += (int64_t)gridDim.x * 256) {
+// One set of rows or two (b.packed null: one).
+__global__ __launch_bounds__(256) void k_mx4_pack_scales(Mx4Unpacked a, Mx4Unpacked b, int blocks, int steps) {
+  const int64_t na = a.count ? *a.count : a.n;
+  const int64_t words_a = (na + 63) / 64 * steps * 64, words = words_a + (b.n + 63) / 64 * steps * 64;
+  for (int64_t w0 = (int64_t)blockIdx.x * 256 + threadIdx.x; w0 < words; w0 += (int64_t)gridDim.x * 256) {
+    const bool second = w0 >= words_a;
+    const int64_t w = second ? w0 - words_a : w0, n = second ? b.n : na;
+    const uint8_t *scales = second ? b.scales : a.scales;
+    const int *list = second ? b.list : a.list;
+    const bool dealt = second ? b.dealt : a.dealt;
     const int lane = (int)(w & 63), i = lane & 15;
     const int64_t gs = w >> 6, g = gs / steps;
     const int block = 4 * (int)(gs - g * steps) + (lane >> 4);
@@ -22,17 +26,15 @@ __global__ __launch_bounds__(256) void k_mx4_pack_scales(const uint8_t *__restri
         const int64_t r = 64 * g + (dealt ? mx4_dealt(t, i) : 16 * t + i);
         if (r < n) v |= (unsigned)scales[(list ? list[r] : r) * blocks + block] << (8 * t);
       }
-    packed[w] = (int)v;
+    (second ? b.packed : a.packed)[w] = (int)v;
   }
 }
 
-hipError_t launch_mx4_pack_scales(hipStream_t stream, const uint8_t *scales, int64_t n, int blocks, bool dealt, int *packed,
-                                  const int *list, const int *count) {
+hipError_t launch_mx4_pack_scales(hipStream_t stream, int blocks, Mx4Unpacked a, Mx4Unpacked b) {
   const int steps = (blocks - 1) / 4 + 1;
-  int64_t grid = ((n + 63) / 64 * steps * 64 + 255) / 256;
+  int64_t grid = ((a.n + 63) / 64 + (b.n + 63) / 64) * steps / 4 + 1;
   if (grid > 4096) grid = 4096;
-  hipLaunchKernelGGL(k_mx4_pack_scales, dim3((unsigned)grid), dim3(256), 0, stream, scales, n, blocks, steps, dealt ? 1 : 0, packed, list,
-                     count);
+  hipLaunchKernelGGL(k_mx4_pack_scales, dim3((unsigned)grid), dim3(256), 0, stream, a, b, blocks, steps);
   return hipGetLastError();
 }
 
@@ -192,8 +194,7 @@ static hipError_t product(som_ctx *c, Mx4Rows a, Mx4Rows b, T *out, int64_t stri
     return hipGetLastError();
   }
   int *pa = static_cast<int *>(scratch), *pb = pa + mx4_packed_bytes(a.n, blocks) / 4;
-  hipError_t e = launch_mx4_pack_scales(c->stream, a.scales, a.n, blocks, false, pa);
-  if (e == hipSuccess) e = launch_mx4_pack_scales(c->stream, b.scales, b.n, blocks, true, pb);
+  const hipError_t e = launch_mx4_pack_scales(c->stream, blocks, Mx4Unpacked{a.scales, a.n, false, pa}, Mx4Unpacked{b.scales, b.n, true, pb});
   if (e != hipSuccess) return e;
   const Mx4Operand oa = {a, pa}, ob = {b, pb};
   // Rows of up to 512 features are bound by the output: two workgroups a CU, one's stores beside the other's products (to bf16, us, wide / low

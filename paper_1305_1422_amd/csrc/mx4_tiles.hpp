@@ -220,7 +220,13 @@ struct Mx4Tile {
 // Words of packed scales: [ceil(n / 64)][steps][64]; lane l's byte t is that of block 4 step + l / 16 of row 64 g + 16 t + l % 16
 // (kDealt: + mx4_dealt(t, l % 16)).
 inline size_t mx4_packed_bytes(int64_t n, int blocks) { return (size_t)((n + 63) / 64) * ((blocks - 1) / 4 + 1) * 256; }
-hipError_t launch_mx4_pack_scales(hipStream_t stream, const uint8_t *scales, int64_t n, int blocks, bool dealt, int *packed,
-                                  const int *list = nullptr, const int *count = nullptr /* device: rows of the list, n of them at most */);
+struct Mx4Unpacked {
+  const uint8_t *scales;
+  int64_t n;
+  bool dealt;
+  int *packed;
+  const int *list, *count;         // or null: the rows that are meant, on the device how many (n of them at most)
+};
+hipError_t launch_mx4_pack_scales(hipStream_t stream, int blocks, Mx4Unpacked a, Mx4Unpacked b = {});
 
 }  // namespace som
