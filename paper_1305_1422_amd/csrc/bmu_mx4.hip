@@ -143,7 +143,7 @@ typedef Mx4Tile<8, 4, 2, 4, true> Mx4Sweep;      // 256 nodes x 256 instances
 
 constexpr int kMx4List = 32;            // groups an instance's list holds (maps of a wide radius came to 23)
 constexpr int kMx4ScanBlocks = 2048;    // workgroups of the exact pass at most
-constexpr int kMx4NodeBlocks = 256;     // workgroups of the node pass at most
+constexpr int kMx4NodeBlocks = 1024;     // workgroups of the node pass at most
 constexpr float kMx4Lowest = -3.0e38f;  // below every score that counts
 
 struct Mx4Counts {
@@ -170,7 +170,6 @@ __global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int co
                                                    char *__restrict__ by_group, int *__restrict__ packed, float *__restrict__ parts, Mx4Counts *__restrict__ counts) {
   __shared__ double s_norm[4][64];
   __shared__ unsigned s_same[4][16];
-  __shared__ float s_max[64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
   const int64_t steps = (blocks - 1) / 4 + 1;
   if (blockIdx.x == 0 && threadIdx.x == 0) *counts = Mx4Counts{0, 0, 0};
@@ -182,18 +181,27 @@ __global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int co
     for (int64_t s = wave; s < steps; s += 4) {
       const int64_t block = 4 * s + q;
       unsigned v = 0;
-      i32x4 x[4];
+      i32x4 x[4], left[4], up[4];
+      int ex[4], eleft[4], eup[4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         const int64_t node = 64 * g + mx4_dealt(t, i);
         const int64_t b = (node < w.n ? node : w.n - 1) * blocks + (block < blocks ? block : blocks - 1);
-        x[t] = *reinterpret_cast<const i32x4 *>(w.codes + b * 16);
-        v |= (unsigned)w.scales[b] << (8 * t);
         // (a node without the other one is compared with itself, and told apart below)
-        const int64_t left = node >= 1 && node < w.n ? b - blocks : b, up = node >= cols && node < w.n ? b - (int64_t)cols * blocks : b;
-        const i32x4 dl = x[t] ^ *reinterpret_cast<const i32x4 *>(w.codes + left * 16), du = x[t] ^ *reinterpret_cast<const i32x4 *>(w.codes + up * 16);
-        if ((dl[0] | dl[1] | dl[2] | dl[3]) != 0 || w.scales[left] != w.scales[b]) same &= ~(1u << t);
-        if ((du[0] | du[1] | du[2] | du[3]) != 0 || w.scales[up] != w.scales[b]) same &= ~(16u << t);
+        const int64_t bl = node >= 1 && node < w.n ? b - blocks : b, bu = node >= cols && node < w.n ? b - (int64_t)cols * blocks : b;
+        x[t] = *reinterpret_cast<const i32x4 *>(w.codes + b * 16);
+        left[t] = *reinterpret_cast<const i32x4 *>(w.codes + bl * 16);
+        up[t] = *reinterpret_cast<const i32x4 *>(w.codes + bu * 16);
+        ex[t] = w.scales[b];
+        eleft[t] = w.scales[bl];
+        eup[t] = w.scales[bu];
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const i32x4 dl = x[t] ^ left[t], du = x[t] ^ up[t];
+        v |= (unsigned)ex[t] << (8 * t);
+        if ((dl[0] | dl[1] | dl[2] | dl[3] | (ex[t] ^ eleft[t])) != 0) same &= ~(1u << t);
+        if ((du[0] | du[1] | du[2] | du[3] | (ex[t] ^ eup[t])) != 0) same &= ~(16u << t);
       }
 #pragma unroll
       for (int t = 0; t < 4; ++t)
@@ -239,12 +247,9 @@ __global__ __launch_bounds__(256) void k_mx4_nodes(Mx4Rows w, int blocks, int co
     }
     __syncthreads();
   }
-  if (threadIdx.x < 64) s_max[threadIdx.x] = most;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int t = 1; t < 64; ++t) most = fmaxf(most, s_max[t]);
-    parts[blockIdx.x] = most;
-  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+  if (threadIdx.x == 0) parts[blockIdx.x] = most;
 }
 
 // ---------------------------------------------------------------- rows of up to 8 steps (1,024 features)
@@ -579,7 +584,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_mx4_resolve(Mx4Rows x, const ch
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q = lane >> 4, steps = (blocks - 1) / 4 + 1;
   const int64_t unit = mx4_stream_bytes(steps), row0 = (int64_t)blockIdx.x * kEach;
   const int mine = x.n - row0 < kEach ? (int)(x.n - row0) : kEach;
-  float wmax2 = (int)threadIdx.x < nparts ? parts[threadIdx.x] : 0.f;
+  float wmax2 = 0.f;
+  for (int t = threadIdx.x; t < nparts; t += kThreads) wmax2 = fmaxf(wmax2, parts[t]);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) wmax2 = fmaxf(wmax2, __shfl_xor(wmax2, o));
   if (lane == 0) s_max[wave] = wmax2;
