@@ -161,7 +161,7 @@ struct Mx4Record {
 // per step the packed scales (mx4_tiles.hpp), then what the accumulators start from in the order of the nodes, rounded up to whole KB.
 __host__ __device__ constexpr int64_t mx4_stream_bytes(int64_t steps) { return steps * 4096 + ((steps + 1) * 256 + 1023) / 1024 * 1024; }
 // By group of 16 nodes besides, for k_mx4_resolve: per step the scales of its fragment, then its 16 starting values (in the stream they share
-// their lines with those of other groups: 126 us instead of 118 for 1e6 instances of 128 features, 80 instead of 76 for 100,000 of 1,000).
+// their lines with those of other groups).
 __host__ __device__ constexpr int64_t mx4_group_bytes(int64_t steps) { return (steps + 1) * 64; }
 
 // A workgroup takes 64 nodes at a time.  parts[blockIdx.x]: the largest |w|^2 it saw (fp64, rounded up to fp32; infinity if it overflows).
@@ -266,8 +266,8 @@ struct Mx4SweepShape {
   static constexpr int unit = (int)mx4_stream_bytes(kT), stage = kUnits * unit, rest = unit / 1024 - 4 * kT, lds = 2 * stage;
 };
 // F: as many as two wavefronts a SIMD leave registers for (one fewer with the lists to write); from 7 steps on a single wavefront with twice
-// as many (100,000 x 10,000, whole search, us, two wavefronts / one: 384 features 201 / 222, 512 262 / 284, 640 320 / 335, 768 383 / 409,
-// 900 542 / 528, 1,000 597 / 589).
+// as many (100,000 x 10,000, whole search, us, two wavefronts / one: 384 features 201 / 232, 512 251 / 267, 640 302 / 315, 768 360 / 384,
+// 900 485 / 473, 1,000 504 / 498).
 template <int kT, bool kCollect> struct Mx4ShapeOf { typedef Mx4SweepShape<kT, kCollect ? 3 : 4, 1, 2> type; };
 template <bool kCollect> struct Mx4ShapeOf<1, kCollect> { typedef Mx4SweepShape<1, 8, 4, 2> type; };
 template <bool kCollect> struct Mx4ShapeOf<2, kCollect> { typedef Mx4SweepShape<2, kCollect ? 5 : 6, 2, 2> type; };
@@ -850,8 +850,8 @@ static Mx4Layout search_layout(const som_ctx *c, int64_t n) {
 }
 
 // Direct, or on the matrix cores?  What either takes, in us, fitted to measurements (instances, nodes, features, us matrix cores / direct: 1, 2,500,
-// 1,000 31 / 8; 100, 2,500, 1,000 55 / 33; 200 59 / 56; 400 65 / 103; 10,000, 400, 32 44 / 25; 20,000 47 / 45; 30, 40,000, 256 101 / 49; 100 113 / 136;
-// 3,000, 1,000, 128 32 / 48; 300, 300, 4,000 152 / 48; 100,000, 9, 100 35 / 117).
+// 1,000 32 / 7; 100, 2,500, 1,000 49 / 34; 200 62 / 56; 400 68 / 101; 10,000, 400, 32 42 / 23; 20,000 43 / 42; 30, 40,000, 256 111 / 48; 100 114 / 135;
+// 3,000, 1,000, 128 34 / 46; 300, 300, 4,000 152 / 49; 100,000, 9, 100 27 / 115).
 static bool direct_pays(const som_ctx *c, int64_t n) {
   const double blocks = mx4_blocks(c->dim), steps = (mx4_blocks(c->dim) - 1) / 4 + 1;
   const double direct = 8.0 + 2.6e-6 * n * c->k * (blocks + 0.6) + 8e-4 * n;

@@ -79,8 +79,8 @@ __global__ __launch_bounds__(256) void k_mx4_product_few(Mx4Rows a, Mx4Rows b, i
 }
 
 // ---------------------------------------------------------------- tiles
-// A wavefront's results leave through LDS, 16 rows at a time, so that its stores are whole stretches of a row (written as the lanes hold them, 32 or 64
-// bytes of 16 rows an instruction, 50,000 x 10,000 products of 256 features to bf16 took 392 us).  kWidth bytes a lane.
+// A wavefront's results leave through LDS, 16 rows at a time, so that its stores are whole stretches of a row (written as the lanes hold them, 16
+// bytes in each of 16 rows an instruction, 50,000 x 10,000 products of 256 features to bf16 take 281 us instead of 256).  kWidth bytes a lane.
 template <typename T, int kCols, int kWidth>
 __device__ __forceinline__ void mx4_store_rows(const T *block, int pitch, T *__restrict__ out, int64_t stride, int64_t rows, int64_t cols, int lane) {
   constexpr int kEach = kWidth / (int)sizeof(T), kLanes = kCols / kEach, kAtOnce = kLanes < 64 ? 64 / kLanes : 1;
@@ -106,25 +106,21 @@ __device__ __forceinline__ void mx4_store_rows(const T *block, int pitch, T *__r
 constexpr int kMx4Band = 8;
 
 // width: bytes that the rows of the output are aligned to, 16, 4 or 2.
-template <typename T, typename Tile, bool kStretch>
+template <typename T, typename Tile>
 __global__ __launch_bounds__(512, (Tile::kFragB == 2 ? 4 : 2)) void k_mx4_product(Mx4Operand a, Mx4Operand b, int blocks, const void *__restrict__ zero16,
                                                      T *__restrict__ out, int64_t stride, unsigned tiles_j, int width) {
   constexpr int kCols = 16 * Tile::kFragA, kPitch = kCols + 16 / (int)sizeof(T);
   __shared__ __attribute__((aligned(16))) char smem[Tile::kLds];
   static_assert(Tile::kWaves * 16 * kPitch * (int)sizeof(T) <= Tile::kLds, "the results of 16 rows of every wavefront");
   Tile t;
-  // Workgroups are dealt to the eight XCDs in turn.  Where the output is most of the work each XCD gets a stretch of consecutive tiles, kMx4Band
-  // rows of tiles column by column, so that the lines of the output that two tiles share meet in one L2 and so do the operands (to bf16, us, as
-  // dealt / stretches of rows of tiles / in bands: 50,000 x 10,000 x 256 371 / 321 / 254, 384 - / 378 / 308; but 8,192 x 8,192 x 4,096 163 / 174 / 172).
-  unsigned ti = blockIdx.x / tiles_j, tj = blockIdx.x - ti * tiles_j;
-  if (kStretch) {
-    const unsigned share = gridDim.x / 8, spare = gridDim.x % 8, x = blockIdx.x % 8;
-    const unsigned tile = x * share + (x < spare ? x : spare) + blockIdx.x / 8;
-    const unsigned band = tile / (kMx4Band * tiles_j), in_band = tile - band * kMx4Band * tiles_j;
-    const unsigned high = min((unsigned)kMx4Band, gridDim.x / tiles_j - band * kMx4Band);
-    tj = in_band / high;
-    ti = band * kMx4Band + in_band - tj * high;
-  }
+  // Workgroups are dealt to the eight XCDs in turn.  Each XCD gets a stretch of consecutive tiles, kMx4Band rows of tiles column by column, so that the
+  // lines of the output that two tiles share meet in one L2 and so do the operands (us, as dealt / row by row of tiles / in bands: to bf16, 50,000 x 10,000
+  // x 256 326 / 323 / 247, 20,000 x 10,000 x 1,000 212 / 198 / 187, 8,192 x 8,192 x 4,096 160 / 172 / 160; to fp32, 100,000 x 2,500 x 1,000 456 / - / 377).
+  const unsigned share = gridDim.x / 8, spare = gridDim.x % 8, xcd = blockIdx.x % 8;
+  const unsigned tile = xcd * share + (xcd < spare ? xcd : spare) + blockIdx.x / 8;
+  const unsigned band = tile / (kMx4Band * tiles_j), in_band = tile - band * kMx4Band * tiles_j;
+  const unsigned high = min((unsigned)kMx4Band, gridDim.x / tiles_j - band * kMx4Band);
+  const unsigned tj = in_band / high, ti = band * kMx4Band + in_band - tj * high;
   t.setup(smem, b, a, nullptr, blocks, zero16);
   const int64_t i0 = (int64_t)ti * Tile::kRowsB, j0 = (int64_t)tj * Tile::kRowsA + t.wa * kCols;
   t.tile_b(i0, a.rows.n, nullptr);
@@ -164,7 +160,7 @@ size_t mx4_product_bytes(const som_ctx *c, int64_t n, int64_t m) {
   return n <= kFewRows ? 0 : mx4_packed_bytes(n, blocks) + mx4_packed_bytes(m, blocks);
 }
 
-template <typename T, typename Tile, bool kStretch>
+template <typename T, typename Tile>
 static hipError_t product_tiles(som_ctx *c, Mx4Operand a, Mx4Operand b, T *out, int64_t stride) {
   const int blocks = mx4_blocks(c->dim);
   const int64_t tj = tiles(b.rows.n, Tile::kRowsA), ti = tiles(a.rows.n, Tile::kRowsB);
@@ -179,7 +175,7 @@ static hipError_t product_tiles(som_ctx *c, Mx4Operand a, Mx4Operand b, T *out, 
     part.rows.n = a.rows.n - i0;
     part.packed += (size_t)(i0 / 64) * ((blocks - 1) / 4 + 1) * 64;
     const dim3 grid((unsigned)(now * tj));
-    hipLaunchKernelGGL((k_mx4_product<T, Tile, kStretch>), grid, dim3(Tile::kThreads), 0, c->stream, part, b, blocks, c->zero16, out + i0 * stride, stride,
+    hipLaunchKernelGGL((k_mx4_product<T, Tile>), grid, dim3(Tile::kThreads), 0, c->stream, part, b, blocks, c->zero16, out + i0 * stride, stride,
                        (unsigned)tj, width);
   }
   return hipGetLastError();
@@ -198,10 +194,10 @@ static hipError_t product(som_ctx *c, Mx4Rows a, Mx4Rows b, T *out, int64_t stri
   if (e != hipSuccess) return e;
   const Mx4Operand oa = {a, pa}, ob = {b, pb};
   // Rows of up to 512 features are bound by the output: two workgroups a CU, one's stores beside the other's products (to bf16, us, wide / low
-  // tiles: 50,000 x 10,000 x 128 261 / 227, 256 295 / 254, 384 347 / 308, 20,000 x 10,000 x 500 151 / 146, 1,000 196 / 202).
+  // tiles: 50,000 x 10,000 x 128 255 / 216, 256 290 / 247, 384 338 / 282, 20,000 x 10,000 x 500 145 / 141, 1,000 187 / 208).
   if (tiles(a.n, Mx4Wide::kRowsB) * tiles(b.n, Mx4Wide::kRowsA) >= c->n_cu)
-    return blocks <= 16 ? product_tiles<T, Mx4Low, true>(c, oa, ob, out, stride) : product_tiles<T, Mx4Wide, false>(c, oa, ob, out, stride);
-  return product_tiles<T, Mx4Narrow, false>(c, oa, ob, out, stride);
+    return blocks <= 16 ? product_tiles<T, Mx4Low>(c, oa, ob, out, stride) : product_tiles<T, Mx4Wide>(c, oa, ob, out, stride);
+  return product_tiles<T, Mx4Narrow>(c, oa, ob, out, stride);
 }
 
 hipError_t launch_mx4_product(som_ctx *c, Mx4Rows a, Mx4Rows b, void *out, int type, int64_t stride, void *scratch) {
