@@ -679,13 +679,14 @@ __global__ __launch_bounds__(kThreads, 4) void k_mx4_resolve(Mx4Rows x, const ch
       for (int r = 0; r < kBatch; ++r)
         if (group == g[r]) mine4 = acc[r];
     }
-    float b = mine4[0], second = kMx4Lowest;
+    float b = kMx4Lowest, second = kMx4Lowest;
     int at = 4 * q;
 #pragma unroll
-    for (int u = 1; u < 4; ++u) {
-      second = fmaxf(second, fminf(b, mine4[u]));
-      at = mine4[u] > b ? 4 * q + u : at;
-      b = fmaxf(b, mine4[u]);
+    for (int u = 0; u < 4; ++u) {
+      const float m = fmaxf(mine4[u], kMx4Lowest);       // (not of a node with a NaN)
+      second = fmaxf(second, fminf(b, m));
+      at = m > b ? 4 * q + u : at;
+      b = fmaxf(b, m);
     }
 #pragma unroll
     for (int o = 16; o < 64; o <<= 1) {
@@ -898,10 +899,24 @@ static Mx4SearchScratch search_scratch(const som_ctx *c, int64_t n, const Mx4Lay
   return m;
 }
 
-size_t mx4_search_bytes(const som_ctx *c, int64_t n) {
+// A search takes at most kMx4AtOnce instances at a time, in equal parts: its scratch stays below a gigabyte (besides the nodes') however large the
+// set.  The first instance too many costs 6 % on rows as short as this matters for (4,194,304 x 32 on 900 nodes 494 us, one more 521).
+constexpr int64_t kMx4AtOnce = 1 << 22;
+static int64_t part_of(int64_t n) {
+  const int64_t parts = (n + kMx4AtOnce - 1) / kMx4AtOnce;
+  return (n + parts - 1) / parts;
+}
+
+static size_t part_bytes(const som_ctx *c, int64_t n) {
   if (!direct_pays(c, n)) return search_scratch(c, n, search_layout(c, n), nullptr).bytes;
   const int shares = direct_shares(c, n, 1 << direct_lanes_log(mx4_blocks(c->dim)));
   return shares > 1 ? (size_t)n * shares * (sizeof(double) + sizeof(int)) : 0;
+}
+
+size_t mx4_search_bytes(const som_ctx *c, int64_t n) {
+  const int64_t part = part_of(n), last = (n - 1) % part + 1;
+  const size_t a = part_bytes(c, part), b = part_bytes(c, last);
+  return a > b ? a : b;
 }
 
 template <int kT, bool kCollect>
@@ -952,7 +967,7 @@ static void launch_resolve(som_ctx *c, Mx4Rows x, const Mx4Layout &l, const Mx4S
   else launch_resolve_of<256, 64, 8>(c, x, l, m, parts, bmus);
 }
 
-hipError_t launch_bmu_mx4(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int *tickets, int32_t *bmus) {
+static hipError_t search_part(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int *tickets, int32_t *bmus) {
   if (direct_pays(c, x.n)) return search_direct(c, x, w, scratch, tickets, bmus);
   const Mx4Layout l = search_layout(c, x.n);
   const Mx4SearchScratch m = search_scratch(c, x.n, l, scratch);
@@ -975,6 +990,16 @@ hipError_t launch_bmu_mx4(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int *
     hipLaunchKernelGGL(k_mx4_exact<1>, grid, dim3(256), 0, c->stream, x, w, blocks, m.counts, m.list, m.found, m.groups, m.whole,
                        direct_lanes_log(blocks), join, bmus);
   return hipGetLastError();
+}
+
+hipError_t launch_bmu_mx4(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int *tickets, int32_t *bmus) {
+  const int64_t part = part_of(x.n), blocks = mx4_blocks(c->dim);
+  for (int64_t r0 = 0; r0 < x.n; r0 += part) {
+    const Mx4Rows rows = {x.codes + r0 * blocks * 16, x.scales + r0 * blocks, x.n - r0 < part ? x.n - r0 : part};
+    const hipError_t e = search_part(c, rows, w, scratch, tickets, bmus + r0);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace som

@@ -218,7 +218,7 @@ class Som:
 
     def train(self, data, n_epochs: int, radius0: float = 0.0, radiusN: float = 0.0, scale0: float = 0.0,
               scaleN: float = 0.0, cooling: str = "linear", bmus: Optional[torch.Tensor] = None):
-        bmus = self._new_bmus(data) if bmus is None else bmus
+        bmus = self._bmus_mx4(data, bmus) if _is_mx4(data) else self._new_bmus(data) if bmus is None else bmus
         self._register(data)
         capi.som_train(self.ctx, n_epochs, radius0, radiusN, scale0, scaleN, COOLING[cooling], self.codebook, bmus)
         return bmus

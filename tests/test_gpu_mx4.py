@@ -296,13 +296,13 @@ def test_search_of_zeros(n):
 
 
 @pytest.mark.parametrize("n,k,dim,rows", [(65_537, 17_001, 40, 1), (66_000, 900, 300, 30), (90_001, 400, 1_100, 1), (262_145, 2_500, 64, 50),
-                                          (270_000, 17_000, 33, 10), (300_007, 300, 200, 3)])
+                                          (270_000, 17_000, 33, 10), (300_007, 300, 200, 3), (5_000_003, 50, 10, 5)])
 def test_search_of_many(n, k, dim, rows):
     """As many instances as are put in order among one another, with ties, copies, NaN and zeros among them."""
     gen = torch.Generator(device="cuda").manual_seed(n)
     w, x = torch.randn(k, dim, generator=gen, device="cuda"), torch.randn(n, dim, generator=gen, device="cuda")
     w[5::7] = w[2::7][:len(w[5::7])].clone()                # equal nodes in other groups,
-    w[16:24] = w[24:32]                                     # and in the same one
+    w[16:20] = w[20:24]                                     # and in the same one
     x[100:40_000] = w[torch.randint(0, k, (39_900,), generator=gen, device="cuda")]
     x[40_000:50_000] = w[33] + 0.01 * x[40_000:50_000]      # all of one node
     x[50_000:50_100] = 0.0
@@ -312,12 +312,13 @@ def test_search_of_many(n, k, dim, rows):
     got = som.bmus(x, nodes=w).long()
     xv, wv = som.dequantize_mx4(x).double(), som.dequantize_mx4(w).double()
     half, at = 0.5 * (wv * wv).sum(1), torch.arange(k, device="cuda")
-    for i in range(0, n, 8192):
-        part = xv[i:i + 8192]
+    step = 8192 if k > 100 else 1 << 20
+    for i in range(0, n, step):
+        part = xv[i:i + step]
         s = part @ wv.T - half                              # (exact: numbers of a kind, few bits)
         want = torch.where(s == s.max(1, keepdim=True).values, at, k).min(1).values
         want[part.isnan().any(1)] = 0
-        assert torch.equal(got[i:i + 8192], want), i
+        assert torch.equal(got[i:i + step], want), i
     som.close()
 
 
@@ -595,6 +596,8 @@ def test_refusals():
         som.bmus(x, nodes=mx)
     with pytest.raises(ValueError):
         som.bmus(mx, bmus=b[:9])
+    with pytest.raises(ValueError):
+        som.train(mx, 1, bmus=b[:9])
     with pytest.raises(ValueError):
         som.products_mx4(mx, mx, out=torch.empty(10, 9, device="cuda"))
     with pytest.raises(ValueError):
