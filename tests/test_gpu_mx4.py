@@ -195,7 +195,8 @@ def check_search(x, w, dim, rows=1):
 
 SIZES = [(1, 1, 1), (1, 3, 40), (5, 64, 32), (17, 65, 33), (64, 16, 128), (100, 400, 10), (65, 130, 129), (300, 77, 1000), (1000, 1025, 100),
          (1, 2500, 1000), (3, 5000, 96), (2000, 63, 257), (4099, 640, 128), (513, 2000, 1024), (700, 900, 1100), (130, 300, 4096),
-         (5000, 3000, 33), (255, 3001, 1000), (2049, 1500, 300), (257, 1025, 4096), (9000, 70, 500), (70, 9000, 500), (3000, 5000, 20)]
+         (5000, 3000, 33), (255, 3001, 1000), (2049, 1500, 300), (257, 1025, 4096), (9000, 70, 500), (70, 9000, 500), (3000, 5000, 20), (70_000, 1, 40),
+         (300, 1, 2_000), (2_000, 2, 1_300), (400, 300, 20_001), (2, 3, 60_000), (1, 40_000, 1)]
 
 
 @pytest.mark.parametrize("n,k,dim", SIZES)
@@ -350,7 +351,9 @@ def test_search_quantises_the_code_book_where_no_nodes_are_given():
 EPOCHS = [(1, 4, 5, 3, "planar", "square", 2.0), (1000, 20, 20, 10, "planar", "square", 3.0), (37, 9, 11, 77, "toroid", "hexagonal", 1.5),
           (3000, 6, 7, 128, "planar", "hexagonal", 2.5), (2500, 40, 35, 100, "toroid", "square", 5.0), (600, 10, 10, 1000, "planar", "square", 1.0),
           (500, 8, 8, 2100, "planar", "square", 2.0),
-          (20000, 30, 40, 64, "toroid", "hexagonal", 3.0)]
+          (20000, 30, 40, 64, "toroid", "hexagonal", 3.0),
+          (1, 1, 1, 5, "planar", "square", 1.0), (2, 1, 7, 33, "toroid", "square", 0.5), (70_000, 5, 6, 40, "planar", "hexagonal", 0.3),
+          (66_000, 90, 100, 20, "planar", "square", 40.0)]
 
 
 @pytest.mark.parametrize("n,rows,cols,dim,map_type,grid_type,radius", EPOCHS)
