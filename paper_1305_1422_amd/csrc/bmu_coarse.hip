@@ -15,6 +15,7 @@
 // so the minima need no exchange between wavefronts.  Tile loads, swizzle and grid decoding are those of
 // bmu_dense_h.hip.
 #include "bmu_dense_common.hpp"
+#include "lds_load.hpp"
 
 namespace som {
 
@@ -26,26 +27,6 @@ constexpr int kCTN = 256, kCTI = 256;      // nodes / instances per workgroup ti
 constexpr int kCThreads = 512;
 
 __device__ __forceinline__ unsigned lds_address_c(const float *p) { return (unsigned)(size_t)(lptr_c_t)p; }
-
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-// Direct-to-LDS load of 16 bytes per lane, "wavefront-uniform base + 32-bit byte offset per lane" form
-// (see bmu_dense_dl.hip for why this is inline assembly).
-__device__ __forceinline__ void load16_to_lds_c(const void *base, unsigned lane_offset, unsigned lds_base) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
-               :
-               : "v"(lane_offset), "s"(base), "s"(lds_base)
-               : "memory", "m0");
-}
-// The same for 4 bytes per lane: lane l's word goes to LDS byte address lds_base + 4 l.
-__device__ __forceinline__ void load4_to_lds_c(const void *base, unsigned lane_offset, unsigned lds_base) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dword %0, %1"
-               :
-               : "v"(lane_offset), "s"(base), "s"(lds_base)
-               : "memory", "m0");
-}
-
-#pragma clang diagnostic pop
 
 __device__ __forceinline__ f16x8 as_halves_c(f32x4 v) { return __builtin_bit_cast(f16x8, v); }
 
@@ -95,7 +76,7 @@ __device__ __forceinline__ void coarse_in_subspace(const CoarseSubspace &sub, fl
     const int last = k - 1 - (nb_first + t) * kCTN;
 #pragma unroll
     for (int i = 0; i < kKS; ++i)
-      load16_to_lds_c(base, (unsigned)min(row[i], last) * (kSub * 2) + slot[i], lds_at + (t % kStages) * kTileBytes + i * 1024);
+      load16_to_lds_at(base, (unsigned)min(row[i], last) * (kSub * 2) + slot[i], lds_at + (t % kStages) * kTileBytes + i * 1024);
   };
   f16x8 h[2][kKS];
   float factor[2];
@@ -236,18 +217,18 @@ __global__ __launch_bounds__(kCThreads, 1) void k_bmu_coarse(CoarseOperands op, 
       // last one is read again: either +inf, or a block of the table that is not written at all
       if (wave < 4) {
         const int node = min(ld_nb * kCTN + wave * 64 + lane, k_const - 1);
-        load4_to_lds_c(wc, (unsigned)node * 4u, lds_wn + ((ld_nb - nb_first) & 1) * (kCTN * 4) + wave * 256);
+        load4_to_lds_at(wc, (unsigned)node * 4u, lds_wn + ((ld_nb - nb_first) & 1) * (kCTN * 4) + wave * 256);
       }
     }
     const unsigned off = (unsigned)ld_kc * (kCRow * 4);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) load16_to_lds_c(wbase + off, woff[i], lds_w + buf * (kCTN * kCRow * 4) + i * 1024);
+    for (int i = 0; i < 4; ++i) load16_to_lds_at(wbase + off, woff[i], lds_w + buf * (kCTN * kCRow * 4) + i * 1024);
     if (!x_stays) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) load16_to_lds_c(xbase + off, xoff[i], lds_x + buf * (kCTI * kCRow * 4) + i * 1024);
+      for (int i = 0; i < 4; ++i) load16_to_lds_at(xbase + off, xoff[i], lds_x + buf * (kCTI * kCRow * 4) + i * 1024);
     } else if (ld_nb == nb_first) {                               // chunk kc of the instance tile lives in sX[kc]
 #pragma unroll
-      for (int i = 0; i < 4; ++i) load16_to_lds_c(xbase + off, xoff[i], lds_x + ld_kc * (kCTI * kCRow * 4) + i * 1024);
+      for (int i = 0; i < 4; ++i) load16_to_lds_at(xbase + off, xoff[i], lds_x + ld_kc * (kCTI * kCRow * 4) + i * 1024);
     }
     if (++ld_kc == nK) { ld_kc = 0; ++ld_nb; }
   };

@@ -15,6 +15,7 @@
 // chunk that belongs at its LDS position.  Rows and columns outside the matrices are read from
 // a 16-byte block of zeros.
 #include "bmu_dense_common.hpp"
+#include "lds_load.hpp"
 
 namespace som {
 
@@ -24,19 +25,6 @@ constexpr int kTileFloats = kTN * kBK;        // one operand tile in LDS: 128 ro
 static_assert(kTN == kTI, "both operand tiles have the same shape");
 
 __device__ __forceinline__ unsigned lds_address(const float *p) { return (unsigned)(size_t)(lptr_t)p; }
-
-// One direct-to-LDS load: lane l's 16 bytes at `g` go to LDS byte address lds_base + 16 l
-// (lds_base wavefront-uniform, passed in M0).  Written as inline assembly on purpose: the
-// compiler would otherwise make every later LDS read wait for these loads, although they fill
-// the buffer that is NOT being read; the ordering that matters is enforced by hand
-// (wait_vector_memory() before the barrier that publishes the buffer).  M0 is a reserved
-// register that the compiler reloads before each use of its own, so overwriting it is safe.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void load16_to_lds(const float *g, unsigned lds_base) {
-  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(g), "s"(lds_base) : "memory", "m0");
-}
-#pragma clang diagnostic pop
 
 __device__ __forceinline__ void wait_vector_memory() {
   // s_waitcnt vmcnt(0): every vector memory operation of this wavefront, the direct-to-LDS

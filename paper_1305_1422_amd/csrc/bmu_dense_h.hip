@@ -28,6 +28,7 @@
 // stream the same instance tile at about the same time, and all but the first find it in that
 // XCD's L2.
 #include "bmu_dense_common.hpp"
+#include "lds_load.hpp"
 
 namespace som {
 
@@ -39,31 +40,6 @@ constexpr int kHWTile = kTN * kHRow;       // floats
 constexpr int kHWI = 2;                    // 64-instance columns of wavefronts in a workgroup
 
 __device__ __forceinline__ unsigned lds_address_h(const float *p) { return (unsigned)(size_t)(lptr_h_t)p; }
-
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-// Direct-to-LDS load of 16 bytes per lane (see bmu_dense_dl.hip for why this is inline assembly),
-// in the addressing form "wavefront-uniform 64-bit base in scalar registers + unsigned 32-bit byte
-// offset per lane": the per-lane offsets are loop constants and the base advances with scalar
-// arithmetic, so a load costs no vector ALU instruction.
-__device__ __forceinline__ void load16_to_lds_h(const void *base, unsigned lane_offset, unsigned lds_base) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
-               :
-               : "v"(lane_offset), "s"(base), "s"(lds_base)
-               : "memory", "m0");
-}
-// The same for 4 bytes per lane: lane l's word goes to LDS byte address lds_base + 4 l.
-__device__ __forceinline__ void load4_to_lds_h(const void *base, unsigned lane_offset, unsigned lds_base) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dword %0, %1"
-               :
-               : "v"(lane_offset), "s"(base), "s"(lds_base)
-               : "memory", "m0");
-}
-// 16 bytes per lane from a full 64-bit address per lane (rows gathered through an index list).
-__device__ __forceinline__ void load16_to_lds_v(const void *lane_address, unsigned lds_base) {
-  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(lane_address), "s"(lds_base) : "memory", "m0");
-}
-#pragma clang diagnostic pop
 
 enum { kHFilter = 0, kHCollect = 1, kHDump = 2, kHPartial = 3, kHFine = 4 };
 
@@ -186,16 +162,16 @@ __device__ __forceinline__ void bmu_dense_h_unit(const float *__restrict__ Xh, c
       // node constants of the block: wc is padded to whole blocks with +inf (such nodes can never
       // win), so the 128 values are loaded like the tiles, as the oldest operation of the batch
       if (!kPartial && wave < 2)
-        load4_to_lds_h(wc + (int64_t)ld_nb * kTN, wn_off,
+        load4_to_lds_at(wc + (int64_t)ld_nb * kTN, wn_off,
                        lds_wn + __builtin_amdgcn_readfirstlane(ld_ord & 3) * (kTN * 4) + wave * 256);
     }
     const unsigned off = (unsigned)ld_kc * (kHRow * 4);
 #pragma unroll
-    for (int i = 0; i < kWSlots; ++i) load16_to_lds_h(wbase + off, woff[i], lds_w + buf * (kHWTile * 4) + i * 1024);
+    for (int i = 0; i < kWSlots; ++i) load16_to_lds_at(wbase + off, woff[i], lds_w + buf * (kHWTile * 4) + i * 1024);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if (kGather) load16_to_lds_v(xptr[i] + off, lds_x + buf * (kHXTile * 4) + i * 1024);
-      else load16_to_lds_h(xbase + off, xoff[i], lds_x + buf * (kHXTile * 4) + i * 1024);
+      if (kGather) load16_to_lds(xptr[i] + off, lds_x + buf * (kHXTile * 4) + i * 1024);
+      else load16_to_lds_at(xbase + off, xoff[i], lds_x + buf * (kHXTile * 4) + i * 1024);
     }
     if (++ld_kc == nK) {
       ld_kc = 0;

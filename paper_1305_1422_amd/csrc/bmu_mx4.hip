@@ -323,13 +323,13 @@ __global__ __launch_bounds__(256, (Mx4ShapeOf<kT, kCollect>::type::waves)) void 
     for (int u = 0; u < kUnits; ++u)
 #pragma unroll
       for (int s = 0; s < kT; ++s)
-        mx4_load_to_lds_at(src + u * Shape::unit + s * 4096, deal, dst + u * Shape::unit + (4 * s + wave) * 1024);
+        load16_to_lds_at(src + u * Shape::unit + s * 4096, deal, dst + u * Shape::unit + (4 * s + wave) * 1024);
 #pragma unroll
     for (int u = 0; u < (kUnits * Shape::rest + 3) / 4; ++u) {
       int c = 4 * u + wave;                    // (no branch, which would tear the order below apart: the last one more than once)
       if ((kUnits * Shape::rest) % 4 != 0 && c >= kUnits * Shape::rest) c = kUnits * Shape::rest - 1;
       const int off = c / Shape::rest * Shape::unit + kT * 4096 + c % Shape::rest * 1024;
-      mx4_load_to_lds_at(src + off, lane * 16, dst + off);
+      load16_to_lds_at(src + off, lane * 16, dst + off);
     }
   };
   struct Piece {

@@ -12,22 +12,10 @@
 // step j + 2 are issued before the products of step j, one barrier a step.
 #pragma once
 
+#include "lds_load.hpp"
 #include "mx4.hpp"
 
 namespace som {
-
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-// Lane l's 16 bytes at g go to LDS byte lds_base + 16 l.  In assembly because the compiler would make every LDS read wait for loads that fill a
-// buffer nobody reads yet; mx4_wait orders them.
-__device__ __forceinline__ void mx4_load_to_lds(const void *g, unsigned lds_base) {
-  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(g), "s"(lds_base) : "memory", "m0");
-}
-// The same from base + offset, the base in scalar registers.
-__device__ __forceinline__ void mx4_load_to_lds_at(const void *base, int offset, unsigned lds_base) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(lds_base) : "memory", "m0");
-}
-#pragma clang diagnostic pop
 
 typedef __attribute__((address_space(3))) void *mx4_lds_t;
 
@@ -133,26 +121,26 @@ struct Mx4Tile {
     const bool in = 4 * step + q < blocks;
 #pragma unroll
     for (int u = 0; u < kLoadA; ++u)
-      mx4_load_to_lds(in ? src_a[u] + 64 * step : zero, base + (wave * kLoadA + u) * 1024);
+      load16_to_lds(in ? src_a[u] + 64 * step : zero, base + (wave * kLoadA + u) * 1024);
 #pragma unroll
     for (int u = 0; u < kLoadB; ++u)
-      mx4_load_to_lds(in ? src_b[u] + 64 * step : zero, base + kOffB + (wave * kLoadB + u) * 1024);
+      load16_to_lds(in ? src_b[u] + 64 * step : zero, base + kOffB + (wave * kLoadB + u) * 1024);
     if (wave == 0) {
       if (lane < kRowsA / 4) {
         int64_t g = tile * (kRowsA / 64) + lane / 16;
         const int64_t last = (a.rows.n - 1) / 64;
         if (g > last) g = last;
-        mx4_load_to_lds(reinterpret_cast<const char *>(a.packed) + (g * steps + step) * 256 + (lane & 15) * 16, base + kOffScaleA);
+        load16_to_lds(reinterpret_cast<const char *>(a.packed) + (g * steps + step) * 256 + (lane & 15) * 16, base + kOffScaleA);
       }
     } else if (wave == 1) {
       if (lane < kRowsB / 4) {
         int64_t g = group_b + lane / 16;
         const int64_t last = (b.rows.n - 1) / 64;
         if (g > last) g = last;
-        mx4_load_to_lds(reinterpret_cast<const char *>(b.packed) + (g * steps + step) * 256 + (lane & 15) * 16, base + kOffScaleB);
+        load16_to_lds(reinterpret_cast<const char *>(b.packed) + (g * steps + step) * 256 + (lane & 15) * 16, base + kOffScaleB);
       }
     } else if (kInit && wave == 2) {
-      if (lane < kRowsA / 4) mx4_load_to_lds(init + tile * kRowsA + 4 * lane, base + kOffInit);
+      if (lane < kRowsA / 4) load16_to_lds(init + tile * kRowsA + 4 * lane, base + kOffInit);
     }
   }
   // The loads of all steps but the last one issued are in LDS, for this wavefront's part.
