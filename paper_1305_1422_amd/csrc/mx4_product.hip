@@ -166,7 +166,8 @@ static hipError_t product_tiles(som_ctx *c, Mx4Operand a, Mx4Operand b, T *out, 
   const int64_t tj = tiles(b.rows.n, Tile::kRowsA), ti = tiles(a.rows.n, Tile::kRowsB);
   const uintptr_t both = (uintptr_t)out | (uintptr_t)(a.rows.n > 1 ? stride * (int64_t)sizeof(T) : 0);
   const int width = both % 16 == 0 ? 16 : both % 4 == 0 ? 4 : 2;
-  const int64_t most = (1ll << 30) / tj > 0 ? (1ll << 30) / tj : 1;           // tile rows of a launch
+  // tile rows of a launch: HIP takes fewer than 2^32 threads in one (one row of tiles always fits: 65 rows of 2^31 products do not fit the card)
+  const int64_t fit = ((1ll << 32) - 1) / Tile::kThreads / tj, most = fit > 0 ? fit : 1;
   for (int64_t t0 = 0; t0 < ti; t0 += most) {
     const int64_t now = ti - t0 < most ? ti - t0 : most, i0 = t0 * Tile::kRowsB;
     Mx4Operand part = a;
