@@ -690,27 +690,32 @@ __global__ __launch_bounds__(256) void k_combine_groups(const int32_t *__restric
 // than kCombineGroup chunks: the group sums k_combine_groups left in every kCombineGroup-th row), eight
 // interleaved running sums (term t goes to sum t mod 8) combined pairwise at the end: a fixed order, with
 // eight loads in flight instead of one.
-__global__ __launch_bounds__(256) void k_combine_chunks(const int32_t *__restrict__ chunk_off, int dim,
+__global__ __launch_bounds__(256) void k_combine_chunks(const int32_t *__restrict__ chunk_off, int k, int dim,
                                                         const float *__restrict__ partial, float *__restrict__ S) {
-  const int b = blockIdx.x;
-  const int c0 = chunk_off[b], nc = chunk_off[b + 1] - c0;
-  if (nc == 1) return;
-  float *dst = S + (int64_t)b * dim;
-  const bool grouped = nc > kCombineGroup;
-  const int terms = grouped ? (nc + kCombineGroup - 1) / kCombineGroup : nc;
-  const int64_t step = (int64_t)(grouped ? kCombineGroup : 1) * dim;
-  const float *src = partial + (int64_t)c0 * dim;
-  // grid.y splits the columns: late in training a few dozen nodes hold all the chunks
-  for (int c = blockIdx.y * blockDim.x + threadIdx.x; c < dim; c += gridDim.y * blockDim.x) {
-    double a[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    int t = 0;
-    for (; t + 8 <= terms; t += 8)
+  for (int b = blockIdx.x; b < k; b += gridDim.x) {
+    const int c0 = chunk_off[b], nc = chunk_off[b + 1] - c0;
+    if (nc == 1) continue;
+    float *dst = S + (int64_t)b * dim;
+    const bool grouped = nc > kCombineGroup;
+    const int terms = grouped ? (nc + kCombineGroup - 1) / kCombineGroup : nc;
+    const int64_t step = (int64_t)(grouped ? kCombineGroup : 1) * dim;
+    const float *src = partial + (int64_t)c0 * dim;
+    // grid.y splits the columns: late in training a few dozen nodes hold all the chunks
+    for (int c = blockIdx.y * blockDim.x + threadIdx.x; c < dim; c += gridDim.y * blockDim.x) {
+      double a[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+      int t = 0;
+      for (; t + 8 <= terms; t += 8)
 #pragma unroll
-      for (int u = 0; u < 8; ++u) a[u] += (double)src[(t + u) * step + c];
-    for (int u = 0; t < terms; ++t, ++u) a[u] += (double)src[t * step + c];
-    dst[c] = (float)(((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7])));
+        for (int u = 0; u < 8; ++u) a[u] += (double)src[(t + u) * step + c];
+      for (int u = 0; t < terms; ++t, ++u) a[u] += (double)src[t * step + c];
+      dst[c] = (float)(((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7])));
+    }
   }
 }
+
+// Workgroups of the launches that have one for every node: of 256 threads HIP takes fewer than 2^24, the largest map's nodes.
+constexpr int kNodeBlocks = 1 << 23;
+static unsigned node_blocks(const som_ctx *c) { return (unsigned)(c->k < kNodeBlocks ? c->k : kNodeBlocks); }
 
 // ---------------------------------------------------------------- sparse rows
 // S_b for CSR data.
@@ -754,12 +759,13 @@ constexpr int64_t kTileFrom = 2, kTilesMax = 32, kCsrFill = 6, kCsrFewEntries = 
 static_assert(kCsrChunkRows % kChunkRows == 0, "the chunk tables are sized for kChunkRows");
 
 // Clears the rows of S whose node has more than `lo` instances.
-__global__ __launch_bounds__(256) void k_zero_rows_if(const int32_t *__restrict__ counts, int lo, int dim,
+__global__ __launch_bounds__(256) void k_zero_rows_if(const int32_t *__restrict__ counts, int k, int lo, int dim,
                                                       float *__restrict__ S) {
-  const int b = blockIdx.x;
-  if (counts[b] <= lo) return;
-  float *dst = S + (int64_t)b * dim;
-  for (int c = blockIdx.y * 256 + threadIdx.x; c < dim; c += gridDim.y * 256) dst[c] = 0.f;
+  for (int b = blockIdx.x; b < k; b += gridDim.x) {
+    if (counts[b] <= lo) continue;
+    float *dst = S + (int64_t)b * dim;
+    for (int c = blockIdx.y * 256 + threadIdx.x; c < dim; c += gridDim.y * 256) dst[c] = 0.f;
+  }
 }
 
 // A lane holds the bounds of one row of the batch at hand, kEach rows to a wavefront, which keeps entries lane and lane + 64 of its own; what lies
@@ -1029,7 +1035,7 @@ static hipError_t launch_combine(som_ctx *c, int64_t max_chunks) {
   if (max_chunks > kCombineGroup)
     hipLaunchKernelGGL(k_combine_groups, dim3((unsigned)(max_chunks < 16 * c->n_cu ? max_chunks : 16 * c->n_cu), ysplit), dim3(cthreads), 0, c->stream, c->chunk_off,
                        c->chunk_node, c->k, c->dim, c->partial);
-  hipLaunchKernelGGL(k_combine_chunks, dim3(c->k, ysplit), dim3(256), 0, c->stream, c->chunk_off, c->dim, c->partial,
+  hipLaunchKernelGGL(k_combine_chunks, dim3(node_blocks(c), ysplit), dim3(256), 0, c->stream, c->chunk_off, c->k, c->dim, c->partial,
                      c->S);
   return hipGetLastError();
 }
@@ -1160,7 +1166,7 @@ hipError_t launch_accumulate_csr(som_ctx *c, const int64_t *indptr, const int32_
     hipError_t e = launch_group_by_bmu(c, bmus, n, rows);
     if (e != hipSuccess) return e;
     if (c->GxT) {          // matrix smoothing only reads the rows of chosen nodes
-      hipLaunchKernelGGL(k_zero_rows_if, dim3(c->k, ysplit), dim3(256), 0, c->stream, c->counts, rows, c->dim, c->S);
+      hipLaunchKernelGGL(k_zero_rows_if, dim3(node_blocks(c), ysplit), dim3(256), 0, c->stream, c->counts, c->k, rows, c->dim, c->S);
     } else {               // the stencil smoothing reads every row: those of nodes nobody chose must be zero
       e = launch_fill_zero_u32(c->stream, c->S, k * c->dim);
       if (e != hipSuccess) return e;
@@ -1187,7 +1193,7 @@ hipError_t launch_accumulate_csr(som_ctx *c, const int64_t *indptr, const int32_
   if (cb > (int64_t)c->n_cu * 16) cb = (int64_t)c->n_cu * 16;
   hipLaunchKernelGGL(k_count_bmus, dim3((unsigned)cb), dim3(256), 0, c->stream, bmus, n, c->k, c->counts);
   if (c->GxT) {
-    hipLaunchKernelGGL(k_zero_rows_if, dim3(c->k, ysplit), dim3(256), 0, c->stream, c->counts, 0, c->dim, c->S);
+    hipLaunchKernelGGL(k_zero_rows_if, dim3(node_blocks(c), ysplit), dim3(256), 0, c->stream, c->counts, c->k, 0, c->dim, c->S);
   } else {
     e = launch_fill_zero_u32(c->stream, c->S, (int64_t)c->k * c->dim);
     if (e != hipSuccess) return e;
