@@ -899,12 +899,22 @@ static Mx4SearchScratch search_scratch(const som_ctx *c, int64_t n, const Mx4Lay
   return m;
 }
 
-// A search takes at most kMx4AtOnce instances at a time, in equal parts: its scratch stays below a gigabyte (besides the nodes') however large the
-// set.  The first instance too many costs 6 % on rows as short as this matters for (4,194,304 x 32 on 900 nodes 494 us, one more 521).
-constexpr int64_t kMx4AtOnce = 1 << 22;
-static int64_t part_of(int64_t n) {
-  const int64_t parts = (n + kMx4AtOnce - 1) / kMx4AtOnce;
-  return (n + parts - 1) / parts;
+// A search takes its instances in equal parts, of at most kMx4AtOnce instances and so many that what grows with them (168 bytes each, of rows of
+// more than 1,024 features 192 and four for every 128) is at most kMx4PartBytes: its scratch stays bounded, besides the nodes', however large
+// the set and long the rows.  The first instance too many costs 6 % on rows as short as this matters for (4,194,304 x 32 on 900 nodes 494 us, one more
+// 521).
+constexpr int64_t kMx4AtOnce = 1 << 22, kMx4PartBytes = 1 << 30;
+static int64_t part_of(const som_ctx *c, int64_t n) {
+  int64_t parts = (n + kMx4AtOnce - 1) / kMx4AtOnce;
+  for (;;) {
+    const int64_t part = (n + parts - 1) / parts;
+    if (part <= 4096 || direct_pays(c, part)) return part;
+    const Mx4Layout l = search_layout(c, part);
+    const int64_t each = (int64_t)l.records * sizeof(Mx4Record) + (4 + kMx4List) * 4 + (l.sweep ? 0 : mx4_packed_bytes(64, mx4_blocks(c->dim)) / 64);
+    if (part * each <= kMx4PartBytes) return part;
+    const int64_t wanted = (n * each + kMx4PartBytes - 1) / kMx4PartBytes;
+    parts = wanted > parts ? wanted : parts + 1;
+  }
 }
 
 static size_t part_bytes(const som_ctx *c, int64_t n) {
@@ -914,7 +924,7 @@ static size_t part_bytes(const som_ctx *c, int64_t n) {
 }
 
 size_t mx4_search_bytes(const som_ctx *c, int64_t n) {
-  const int64_t part = part_of(n), last = (n - 1) % part + 1;
+  const int64_t part = part_of(c, n), last = (n - 1) % part + 1;
   const size_t a = part_bytes(c, part), b = part_bytes(c, last);
   return a > b ? a : b;
 }
@@ -993,7 +1003,7 @@ static hipError_t search_part(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, i
 }
 
 hipError_t launch_bmu_mx4(som_ctx *c, Mx4Rows x, Mx4Rows w, void *scratch, int *tickets, int32_t *bmus) {
-  const int64_t part = part_of(x.n), blocks = mx4_blocks(c->dim);
+  const int64_t part = part_of(c, x.n), blocks = mx4_blocks(c->dim);
   for (int64_t r0 = 0; r0 < x.n; r0 += part) {
     const Mx4Rows rows = {x.codes + r0 * blocks * 16, x.scales + r0 * blocks, x.n - r0 < part ? x.n - r0 : part};
     const hipError_t e = search_part(c, rows, w, scratch, tickets, bmus + r0);

@@ -51,3 +51,32 @@ def test_quantisation_of_more_blocks_than_a_launch_holds():
     assert not mx.codes[:, 1:].any()
     assert torch.equal(som.dequantize_mx4(mx, torch.bfloat16), x)
     som.close()
+
+
+@pytest.mark.parametrize("n,dim", [(1 << 21, 16_384), (5_000_003, 1_100)])
+def test_scratch_of_a_search_is_bounded(n, dim):
+    """Rows for which a search of all at once would take 1.4 and 1.1 GB besides the nodes: it is made in parts, and finds the same nodes."""
+    from paper_1305_1422_amd import Mx4, Som
+    k, kinds, blocks = 3, 1000, (dim + 31) // 32
+    gen = torch.Generator(device="cuda").manual_seed(dim)
+    few = torch.randint(0, 256, (kinds, 16 * blocks), dtype=torch.uint8, device="cuda", generator=gen)
+    if dim % 32:
+        few[:, 16 * (blocks - 1) + dim % 32 // 2:] = 0        # (an even number of features: whole bytes)
+    which = torch.randint(0, kinds, (n,), device="cuda", generator=gen)
+    x = Mx4(torch.empty((n, 16 * blocks), dtype=torch.uint8, device="cuda"), torch.full((n, blocks), 127, dtype=torch.uint8, device="cuda"))
+    torch.index_select(few, 0, which, out=x.codes)
+    w = Mx4(few[:k].flip(1).contiguous() if dim % 32 == 0 else few[k:2 * k].clone(), torch.full((k, blocks), 126, dtype=torch.uint8, device="cuda"))
+    som = Som(1, k, dim, seed=1)
+    xv = som.dequantize_mx4(Mx4(few, x.scales[:kinds].contiguous())).double()
+    wv = som.dequantize_mx4(w).double()
+    score = xv @ wv.T - 0.5 * (wv * wv).sum(1)                # (exact: one scale a side)
+    want = score.argmax(1).int()
+    bmus = torch.empty(n, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    before = torch.cuda.mem_get_info()[0]
+    som.bmus(x, bmus, w)
+    torch.cuda.synchronize()
+    taken = before - torch.cuda.mem_get_info()[0]
+    assert taken <= (1 << 30) + (64 << 20), taken             # (the nodes' part and rounding to pages: a few MB)
+    assert torch.equal(bmus, want[which])
+    som.close()
