@@ -215,9 +215,9 @@ int som_mx4_product(som_ctx *ctx, const uint8_t *codes_a, const uint8_t *scales_
  *   node_codes, node_scales   the rows*cols nodes (som_mx4_quantize of a code book, made once for a map that is searched
  *           often), read only.
  *   bmus    device [n] int32 out: the node whose values are nearest to those of the instance, exact ties to the lowest index.
- * Decided by the distances of the values that both sides stand for: exactly, while the scales of a row's products
- * lie within a factor of 2^40 of each other, beyond that in fp64.  An instance with a NaN block is mapped to node 0, a
- * node with one is never chosen.
+ * Decided by the distances of the values that both sides stand for: exactly, while the products of an instance's scales with
+ * a node's, block by block, and the squares of the node's lie within a factor of 2^39 / B of each other (blocks of zeros aside; 2^34 for
+ * 1,000 features), beyond that in fp64.  An instance with a NaN block is mapped to node 0, a node with one is never chosen.
  *
  * som_update_mx4, som_train_epoch_mx4, som_set_data_mx4 - the batch update, one epoch, and the registration of a
  * training set for som_train and som_train_snapshots, as for dense data.  The code book stays fp32; the search of an

@@ -2,7 +2,9 @@
 // smallest |x - w|^2 = |x|^2 - 2 (x.w - |w|^2 / 2), the lowest of equally near ones.
 //
 // Small searches are direct: every score x.w - |w|^2 / 2 in fp64.  The dot product of two blocks is exact in fp32 (mx4.hpp), the sum over the
-// blocks is taken in fp64, exact while the exponents of a row's products lie within 2^40 of each other.  Groups of lanes share a node's blocks.
+// blocks is taken in fp64.  With M and m the largest and smallest product of scales among x.w and |w|^2, all terms are multiples of m / 8 and their
+// magnitudes add up to B (1152 + 576) M at most: every sum is exact while B 13824 M <= 2^53 m, so for M / m up to 2^39 / B.  Groups of lanes
+// share a node's blocks.
 //
 // Larger ones go through the matrix cores, whose fp32 sums are off by a bound that is known (margin below):
 //   k_mx4_nodes    -|w|^2 / 2 of every node (what the accumulators start from) and the nodes' scales, packed;
