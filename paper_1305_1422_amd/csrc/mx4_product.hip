@@ -195,7 +195,8 @@ static hipError_t product(som_ctx *c, Mx4Rows a, Mx4Rows b, T *out, int64_t stri
   if (e != hipSuccess) return e;
   const Mx4Operand oa = {a, pa}, ob = {b, pb};
   // Rows of up to 512 features are bound by the output: two workgroups a CU, one's stores beside the other's products (to bf16, us, wide / low
-  // tiles: 50,000 x 10,000 x 128 255 / 216, 256 290 / 247, 384 338 / 282, 20,000 x 10,000 x 500 145 / 141, 1,000 187 / 208).
+  // tiles: 50,000 x 10,000 x 128 255 / 216, 256 290 / 247, 384 338 / 282, 20,000 x 10,000 x 500 145 / 141, 1,000 187 / 208; to fp32, 100,000 x 2,500 x
+  // 128 292 / 260, 384 309 / 264, 512 320 / 287, 768 351 / 363, 1,000 378 / 412, 20,000 x 10,000 x 500 204 / 191, 1,000 241 / 261).
   if (tiles(a.n, Mx4Wide::kRowsB) * tiles(b.n, Mx4Wide::kRowsA) >= c->n_cu)
     return blocks <= 16 ? product_tiles<T, Mx4Low>(c, oa, ob, out, stride) : product_tiles<T, Mx4Wide>(c, oa, ob, out, stride);
   return product_tiles<T, Mx4Narrow>(c, oa, ob, out, stride);
