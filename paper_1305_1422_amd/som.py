@@ -239,7 +239,8 @@ class Som:
         return (bmus, um, cbs, ball) if snapshots == 2 else (bmus, um)
 
     def bmu_distances(self, data, bmus: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
-        """(distance of every instance to node bmus[j] [n] fp32, their mean [1] fp64), both on the device."""
+        """(distance of every instance to node bmus[j] [n] fp32, their mean [1] fp64), both on the device.  Dense or CSR data;
+        rows in microscaled 4-bit form are read back first (``dequantize_mx4``)."""
         dist = torch.empty(bmus.shape[0], dtype=torch.float32, device=self.device)
         qe = torch.empty(1, dtype=torch.float64, device=self.device)
         if _is_csr(data):
