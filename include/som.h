@@ -225,7 +225,7 @@ int som_mx4_product(som_ctx *ctx, const uint8_t *codes_a, const uint8_t *scales_
  * code book.  The sums are those of the values that the rows stand for.
  * Scratch: the code book in this form for epochs, once more for searches; per instance of a search 168 bytes, of rows of more than 1,024
  * features 192 and 1/32 byte per feature (3 MB in all for the smallest sets; 2^30 bytes at most: larger sets are searched in parts); for
- * products 1/32 byte per feature of either side.  It grows without waiting: what it replaces is kept until som_destroy, so that recorded
+ * products 1/32 byte per feature of either side.  It grows without waiting, to twice its size at least where there is room: what it replaces is kept until som_destroy, so that recorded
  * searches and products keep theirs (recorded calls share it with one another and with the context's other calls: replays follow each other
  * and those in order, as on the context's stream).  The update's own scratch is that of som_update_dense (a later call with more instances replaces it:
  * record epochs after the largest).  A call that is being recorded into a graph and needs more scratch than any call before it ->
